@@ -442,6 +442,110 @@ sb_status sb_conv_in_wgrad_static(const void* x, const void* dy, float* dw, floa
                                   int32_t W, int32_t Cin, int32_t Cout, int32_t precision, void* stream);
 const char* sb_static_last_error(void);
 
+/*
+ * Operators of a residual gated feed-forward block and of its training, on the caller's own tensors (no counterpart in the paper).
+ *
+ * Common rules: every matrix is dense and row-major, in the activation dtype of `precision` (float or bfloat16); vectors of d elements
+ * (norm weights, gates, scales) and the rows kept between the passes are float.  DEVICE pointers unless stated.  Calls only enqueue
+ * work on `stream` and may be captured into a graph (make the first call on a device outside of a capture: it looks up addresses and raises
+ * kernel limits).  A workspace belongs to its call until the work has run: two calls that run at the same time, replays of graphs
+ * included, need one each.  rows = 0 is a valid call: gradients of weights are then zero.  The bounded waits inside the kernels report
+ * to one status word per device, which sb_ops_check reads.  Errors: return code and sb_last_error().
+ */
+
+/* Synchronises `stream`; SB_ERR_TIMEOUT if an operator's kernel has given up on a bounded wait since the last check (the word is then cleared). */
+sb_status sb_ops_check(void* stream);
+
+/*
+ * Gated feed-forward block:  GU = X Wgu^T, G and U its left and right halves, H = a(G) * U, Y = H Wd^T.
+ *   x [rows, d], w_gate_up [2f, d] (gate rows first), w_down [d, f], y [rows, d]; all 16-byte aligned.
+ *   gu [rows, 2f] : receives GU for the backward pass, or NULL.
+ * Backward, from the gradient dy of Y and the GU kept by the forward call:
+ *   dH = dY Wd, dG = dH U a'(G), dU = dH a(G), dX = [dG dU] Wgu, dWgu = [dG dU]^T X, dWd = dY^T H; any of dx, dw_gate_up and dw_down may be NULL.
+ *   The weight gradients are overwritten, in grad_dtype (SB_DT_F32, or SB_DT_BF16 with SB_BF16).
+ * SB_BF16 sums in float and rounds H, dG and dU to bfloat16 where they become operands of a product.
+ * a' of SB_ACT_RELU is 0 at 0.  SB_ERR_UNSUPPORTED: d or f above 2^20, rows of 2^31 or more.
+ *   ws : workspace of sb_ffn_bytes bytes (backward: 0 or 1), 256-byte aligned.
+ */
+enum { SB_ACT_SILU = 0, SB_ACT_GELU = 1, SB_ACT_RELU = 2 }; /* g / (1 + exp(-g)); g (1 + erf(g / sqrt 2)) / 2; max(g, 0) */
+typedef struct {
+    int64_t rows;
+    int32_t d, f;         /* width, hidden width */
+    int32_t act;          /* SB_ACT_* */
+    int32_t precision;    /* SB_FP32 or SB_BF16 */
+    int32_t grad_dtype;   /* SB_DT_* of the weight gradients */
+} sb_ffn_config;
+sb_status sb_ffn_bytes(const sb_ffn_config* cfg, int32_t backward, size_t* bytes);
+sb_status sb_ffn_forward(const sb_ffn_config* cfg, const void* x, const void* w_gate_up, const void* w_down, void* gu, void* y,
+                         void* ws, size_t ws_bytes, void* stream);
+sb_status sb_ffn_backward(const sb_ffn_config* cfg, const void* dy, const void* x, const void* gu, const void* w_gate_up, const void* w_down,
+                          void* dx, void* dw_gate_up, void* dw_down, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Norms before and after a block, with the block's gate and the residual scale, in one pass:
+ *   y = scale * x + gate * (w_post * N(f)),   n = w_pre * N(y)
+ * x [rows, d]: the residual; f: the block's output; y: the next residual; n: the next block's input.  N(v) = v / sqrt(mean(v^2) + eps)
+ * (SB_NORM_RMS) or (v - mean(v)) / sqrt(var(v) + eps) (SB_NORM_LAYER).  Any part may be missing:
+ *   f NULL      : the norm in front of the first block, y is x (pass y = NULL);  w_post, gate and scale are then NULL too
+ *   w_post NULL : f itself in the place of w_post * N(f);   gate or scale NULL : one;   w_pre NULL : no n (pass n = NULL)
+ *   y NULL      : y is not stored
+ * gate [groups, d]: row r uses gate row r / (rows / groups); groups = 0 without a gate.  w_post, scale, w_pre [d].
+ *   stats [rows, 4] : float, 16-byte aligned, receives what the backward pass needs (mean and 1/deviation of f's and y's rows), or NULL.
+ * Backward, from dy and dn (either may be NULL): dx and df (activation dtype), and the vectors' gradients (float, overwritten; sums over the
+ * rows, dgate over each group's), any of which may be NULL.  y is computed again from x and f.  Same bits on every call.
+ *   ws : workspace of sb_norm_bytes bytes, 16-byte aligned.
+ * SB_ERR_UNSUPPORTED: d above 16384.
+ */
+enum { SB_NORM_RMS = 0, SB_NORM_LAYER = 1 };
+typedef struct {
+    int64_t rows, groups;
+    int32_t d;
+    int32_t kind;         /* SB_NORM_* */
+    int32_t precision;    /* SB_FP32 or SB_BF16 */
+    float eps;
+} sb_norm_config;
+sb_status sb_norm_bytes(const sb_norm_config* cfg, size_t* bytes);
+sb_status sb_norm_forward(const sb_norm_config* cfg, const void* x, const float* w_pre, const void* f, const float* w_post, const float* gate,
+                          const float* scale, void* y, void* n, float* stats, void* stream);
+sb_status sb_norm_backward(const sb_norm_config* cfg, const void* dy, const void* dn, const float* stats, const void* x, const float* w_pre,
+                           const void* f, const float* w_post, const float* gate, const float* scale, void* dx, void* df, float* dw_pre,
+                           float* dw_post, float* dgate, float* dscale, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One AdamW step over a list of tensors, in one kernel for up to 350 of them:
+ *   m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2;  p <- (1 - lr wd) p - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
+ * list (HOST): param float; grad float or bfloat16 (config); shadow: bfloat16 copy of the parameter to refresh, or NULL; n elements.
+ * state_bits 32: m and v float, scales unused.  state_bits 8: m and v one byte per element, m_scale and v_scale one float per 256
+ * consecutive elements (the last block may be shorter), each a power of two:
+ *   m = e4m3(code) * m_scale, rounded to nearest even;  v = u(code) * v_scale, u = five bits of exponent (bias 30; 0: subnormal) and three of
+ *   mantissa, rounded up or down by chance: element e's 16 random bits are half e % 2 (low first) of word e % 8 / 2 of Philox-4x32-10
+ *   at counter {e / 8 (two words), index in the list, step}, key = seed.  Codes 0x7F and 255: not a number.  Zero bytes are zero moments.
+ * step: number of this step, from 1.  For a step replayed in a graph: dev_step (int64) and dev_lr (float), DEVICE words that are read
+ * instead of `step` and `lr` where they are not NULL (the caller changes them between replays).
+ * Tensors of the list must not overlap.  Pointers need their element's alignment; 16 bytes make the accesses wide.
+ * sb_adamw_moments writes what 8-bit moments stand for as bfloat16 (exact) to m_out[i] and v_out[i] (HOST arrays of DEVICE pointers).
+ */
+typedef struct {
+    float* param;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void* shadow;
+    int64_t n;
+} sb_adamw_tensor;
+typedef struct {
+    uint64_t seed;
+    int32_t state_bits;   /* 32 or 8 */
+    int32_t grad_dtype;   /* SB_DT_F32 or SB_DT_BF16 */
+} sb_adamw_config;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const int64_t* dev_step;
+    const float* dev_lr;
+} sb_adamw_hyper;
+sb_status sb_adamw_tensors(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, const sb_adamw_hyper* hyper, int64_t step, void* stream);
+sb_status sb_adamw_moments(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, void* const* m_out, void* const* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
 
@@ -26,6 +26,8 @@ SB_FLAG_INPUT_GRAD, SB_FLAG_FORCE_SIMT, SB_FLAG_PROFILE_LAYERS, SB_FLAG_FORCE_PA
 (SB_T_WEIGHT, SB_T_BIAS, SB_T_GRAD_W, SB_T_GRAD_B, SB_T_MOM_W, SB_T_MOM_B, SB_T_ACT, SB_T_DACT,
  SB_T_POOL_IDX, SB_T_ROW_LOSS, SB_T_INPUT_GRAD, SB_T_SHADOW_W) = range(12)
 SB_DT_F32, SB_DT_BF16, SB_DT_U8, SB_DT_I32 = 0, 1, 2, 3
+SB_ACT_SILU, SB_ACT_GELU, SB_ACT_RELU = 0, 1, 2
+SB_NORM_RMS, SB_NORM_LAYER = 0, 1
 STATUS_NAMES = {0: "SB_OK", 1: "SB_ERR_INVALID_ARG", 2: "SB_ERR_SHAPE", 3: "SB_ERR_UNSUPPORTED",
                 4: "SB_ERR_ARENA_TOO_SMALL", 5: "SB_ERR_CUDA", 6: "SB_ERR_STATE", 7: "SB_ERR_TIMEOUT"}
 
@@ -37,6 +39,28 @@ class sb_layer(ctypes.Structure):
 class sb_config(ctypes.Structure):
     _fields_ = [("H", c_int32), ("W", c_int32), ("C", c_int32), ("batch_per_replica", c_int32),
                 ("R", c_int32), ("K", c_int32), ("precision", c_int32), ("flags", c_int32)]
+
+
+class sb_ffn_config(ctypes.Structure):
+    _fields_ = [("rows", c_int64), ("d", c_int32), ("f", c_int32), ("act", c_int32), ("precision", c_int32), ("grad_dtype", c_int32)]
+
+
+class sb_norm_config(ctypes.Structure):
+    _fields_ = [("rows", c_int64), ("groups", c_int64), ("d", c_int32), ("kind", c_int32), ("precision", c_int32), ("eps", c_float)]
+
+
+class sb_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
+                ("shadow", c_void_p), ("n", c_int64)]
+
+
+class sb_adamw_config(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("state_bits", c_int32), ("grad_dtype", c_int32)]
+
+
+class sb_adamw_hyper(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("weight_decay", c_double),
+                ("dev_step", c_void_p), ("dev_lr", c_void_p)]
 
 
 class sb_plan_node(ctypes.Structure):
@@ -95,6 +119,15 @@ def _load():
         "sb_conv_in_wgrad_static": [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p],
         "sb_partition": [P(sb_layer), c_int32, P(sb_config), P(sb_plan_node), c_int32, P(c_int32)],
         "sb_exchange_plan": [P(sb_layer), c_int32, P(sb_config), P(sb_exchange_msg), c_int32, P(c_int32)],
+        "sb_ops_check": [c_void_p],
+        "sb_ffn_bytes": [P(sb_ffn_config), c_int32, P(c_size_t)],
+        "sb_ffn_forward": [P(sb_ffn_config)] + [c_void_p] * 6 + [c_size_t, c_void_p],
+        "sb_ffn_backward": [P(sb_ffn_config)] + [c_void_p] * 9 + [c_size_t, c_void_p],
+        "sb_norm_bytes": [P(sb_norm_config), P(c_size_t)],
+        "sb_norm_forward": [P(sb_norm_config)] + [c_void_p] * 10,
+        "sb_norm_backward": [P(sb_norm_config)] + [c_void_p] * 16 + [c_size_t, c_void_p],
+        "sb_adamw_tensors": [P(sb_adamw_tensor), c_int32, P(sb_adamw_config), P(sb_adamw_hyper), c_int64, c_void_p],
+        "sb_adamw_moments": [P(sb_adamw_tensor), c_int32, P(sb_adamw_config), P(c_void_p), P(c_void_p), c_void_p],
         "sb_profile_begin": [c_void_p, c_void_p],
         "sb_profile_end": [c_void_p, c_void_p, P(sb_profile_entry), c_int32, P(c_int32)],
     }
@@ -143,6 +176,15 @@ sb_launch_count = _lib.sb_launch_count
 sb_conv_in_wgrad_static = _lib.sb_conv_in_wgrad_static
 sb_profile_begin = _lib.sb_profile_begin
 sb_profile_end = _lib.sb_profile_end
+sb_ops_check = _lib.sb_ops_check
+sb_ffn_bytes = _lib.sb_ffn_bytes
+sb_ffn_forward = _lib.sb_ffn_forward
+sb_ffn_backward = _lib.sb_ffn_backward
+sb_norm_bytes = _lib.sb_norm_bytes
+sb_norm_forward = _lib.sb_norm_forward
+sb_norm_backward = _lib.sb_norm_backward
+sb_adamw_tensors = _lib.sb_adamw_tensors
+sb_adamw_moments = _lib.sb_adamw_moments
 sb_partition = _lib.sb_partition
 sb_exchange_plan = _lib.sb_exchange_plan
 
@@ -199,6 +241,202 @@ def conv_in_wgrad_static(x, dy, dw, db, precision):
                                       c_void_p(torch.cuda.current_stream().cuda_stream))
     if st != SB_OK:
         raise SBError(st, sb_static_last_error())
+
+
+# ---- operators on the caller's own tensors ---------------------------------------------------
+# Dense CUDA tensors of one device; outputs and workspaces come from torch's allocator, on the current stream of that device.
+
+
+def _on_device(t):
+    """(torch, the tensor's device as a context where it is not the current one, its current stream as a pointer)"""
+    import contextlib
+    import torch
+    d = t.device
+    if d.type != "cuda":
+        raise SBError(1, f"the tensors must lie on a CUDA device (got {d})")
+    here = contextlib.nullcontext() if d.index == torch.cuda.current_device() else torch.cuda.device(d)
+    return torch, here, torch._C._cuda_getCurrentRawStream(d.index)
+
+
+def _dense(name, t, shape, dtype, device):
+    """The tensor's address; SBError if it is not what the call needs."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise SBError(1, f"{name}: expected a dense {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)}"
+                         f" {'' if t.is_contiguous() else 'with strides ' + str(t.stride()) + ' '}on {t.device}")
+    return t.data_ptr()
+
+
+def _precision(torch, t):
+    if t.dtype == torch.bfloat16:
+        return SB_BF16
+    if t.dtype == torch.float32:
+        return SB_FP32
+    raise SBError(1, f"x: float32 or bfloat16, not {t.dtype}")
+
+
+def _workspace(torch, nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _ffn_config(torch, x, w_gate_up, w_down, act, grad_dtype=SB_DT_F32):
+    if x.dim() != 2 or w_gate_up.dim() != 2:
+        raise SBError(2, "x and w_gate_up must be matrices")
+    rows, d = x.shape
+    f = w_gate_up.shape[0] // 2
+    _dense("x", x, (rows, d), x.dtype, x.device)
+    c = sb_ffn_config(rows, d, f, act, _precision(torch, x), grad_dtype)
+    return c, _dense("w_gate_up", w_gate_up, (2 * f, d), x.dtype, x.device), _dense("w_down", w_down, (d, f), x.dtype, x.device)
+
+
+def ffn_forward(x, w_gate_up, w_down, act=SB_ACT_SILU, save=False):
+    """Gated feed-forward block: (a(x Wg^T) * (x Wu^T)) Wd^T with w_gate_up = [Wg; Wu].  x [rows, d], w_gate_up [2f, d], w_down [d, f].
+    save: returns (y, gu), gu [rows, 2f] being what ffn_backward needs."""
+    torch, here, stream = _on_device(x)
+    c, wgu, wd = _ffn_config(torch, x, w_gate_up, w_down, act)
+    with here:
+        n = c_size_t()
+        _check(sb_ffn_bytes(byref(c), 0, byref(n)))
+        ws = _workspace(torch, n.value, x.device)
+        y = torch.empty_like(x)
+        gu = torch.empty((c.rows, 2 * c.f), dtype=x.dtype, device=x.device) if save else None
+        _check(sb_ffn_forward(byref(c), x.data_ptr(), wgu, wd, gu.data_ptr() if save else None, y.data_ptr(),
+                              ws.data_ptr() if n.value else None, n.value, stream))
+    return (y, gu) if save else y
+
+
+def ffn_backward(dy, x, gu, w_gate_up, w_down, act=SB_ACT_SILU, grad_dtype=None, needs=(True, True, True)):
+    """(dx, dw_gate_up, dw_down) from the gradient of ffn_forward's y and the gu it kept.  grad_dtype: torch dtype of the weight gradients
+    (default: x's); needs: which of the three to compute (None for the others)."""
+    torch, here, stream = _on_device(x)
+    grad_dtype = x.dtype if grad_dtype is None else grad_dtype
+    if grad_dtype not in (torch.float32, torch.bfloat16):
+        raise SBError(1, f"grad_dtype: float32 or bfloat16, not {grad_dtype}")
+    c, wgu, wd = _ffn_config(torch, x, w_gate_up, w_down, act, SB_DT_BF16 if grad_dtype == torch.bfloat16 else SB_DT_F32)
+    pdy, pgu = _dense("dy", dy, x.shape, x.dtype, x.device), _dense("gu", gu, (c.rows, 2 * c.f), x.dtype, x.device)
+    with here:
+        n = c_size_t()
+        _check(sb_ffn_bytes(byref(c), 1, byref(n)))
+        ws = _workspace(torch, n.value, x.device)
+        dx = torch.empty_like(x) if needs[0] else None
+        dwgu = torch.empty(w_gate_up.shape, dtype=grad_dtype, device=x.device) if needs[1] else None
+        dwd = torch.empty(w_down.shape, dtype=grad_dtype, device=x.device) if needs[2] else None
+        _check(sb_ffn_backward(byref(c), pdy, x.data_ptr(), pgu, wgu, wd, *[None if t is None else t.data_ptr() for t in (dx, dwgu, dwd)],
+                               ws.data_ptr() if n.value else None, n.value, stream))
+    return dx, dwgu, dwd
+
+
+def _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, eps):
+    if x.dim() != 2 or (gate is not None and gate.dim() != 2):
+        raise SBError(2, "x and gate must be matrices")
+    rows, d = x.shape
+    f32, dev = torch.float32, x.device
+    c = sb_norm_config(rows, 0 if gate is None else gate.shape[0], d, kind, _precision(torch, x), eps)
+    return c, [_dense("x", x, (rows, d), x.dtype, dev), _dense("w_pre", w_pre, (d,), f32, dev), _dense("f", f, (rows, d), x.dtype, dev),
+               _dense("w_post", w_post, (d,), f32, dev), _dense("gate", gate, (c.groups, d), f32, dev), _dense("scale", scale, (d,), f32, dev)]
+
+
+def norm_forward(x, w_pre=None, f=None, w_post=None, gate=None, scale=None, kind=SB_NORM_RMS, eps=1e-6, save=False):
+    """y = scale * x + gate * (w_post * N(f)), n = w_pre * N(y): the norms behind one block and in front of the next, with the block's
+    gate ([groups, d], a row for rows / groups rows of x) and the residual scale.  Without f, y is x; without w_pre there is no n.
+    Returns (y, n), and with save (y, n, stats) for norm_backward."""
+    torch, here, stream = _on_device(x)
+    c, ptrs = _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, eps)
+    with here:
+        y = x if f is None else torch.empty_like(x)
+        n = torch.empty_like(x) if w_pre is not None else None
+        stats = torch.empty((c.rows, 4), dtype=torch.float32, device=x.device) if save else None
+        _check(sb_norm_forward(byref(c), *ptrs, None if f is None else y.data_ptr(), None if n is None else n.data_ptr(),
+                               stats.data_ptr() if save else None, stream))
+    return (y, n, stats) if save else (y, n)
+
+
+def norm_backward(dy, dn, stats, x, w_pre=None, f=None, w_post=None, gate=None, scale=None, kind=SB_NORM_RMS):
+    """Gradients of norm_forward from those of y and n (either may be None) as a dict: dx, df, dw_pre, dw_post, dgate, dscale (None where there
+    is no such input; dw_pre also without dn)."""
+    torch, here, stream = _on_device(x)
+    c, ptrs = _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, 0.0)
+    dev = x.device
+    pdy, pdn = _dense("dy", dy, x.shape, x.dtype, dev), _dense("dn", dn, x.shape, x.dtype, dev)
+    pst = _dense("stats", stats, (c.rows, 4), torch.float32, dev)
+    with here:
+        n = c_size_t()
+        _check(sb_norm_bytes(byref(c), byref(n)))
+        ws = _workspace(torch, n.value, dev)
+        out = {"dx": torch.empty_like(x), "df": None if f is None else torch.empty_like(f), "dw_pre": None if dn is None or w_pre is None else torch.empty_like(w_pre),
+               "dw_post": None if w_post is None else torch.empty_like(w_post), "dgate": None if gate is None else torch.empty_like(gate),
+               "dscale": None if scale is None else torch.empty_like(scale)}
+        _check(sb_norm_backward(byref(c), pdy, pdn, pst, *ptrs, *[None if t is None else t.data_ptr() for t in out.values()],
+                                ws.data_ptr() if n.value else None, n.value, stream))
+    return out
+
+
+class AdamW:
+    """AdamW over a list of parameters (float, updated in place) with gradients and moments of the caller's: the moments as float tensors, or in
+    8 bits (m: float8_e4m3fn or uint8, v: uint8, and a float scale for each 256 elements of either).  The tensors are looked at once, here;
+    `grads` may be replaced (set_grads).  shadows: bf16 copies of the parameters, refreshed by every step."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, shadows=None, seed=0):
+        import torch
+        if not params:
+            raise SBError(1, "an empty list of parameters")
+        self._t = (torch, params, m, v, m_scale, v_scale, shadows)
+        n, dev = len(params), params[0].device
+        if not all(len(x) == n for x in (grads, m, v, m_scale, v_scale, shadows) if x is not None):
+            raise SBError(1, "lists of different lengths")
+        bits = 32 if m_scale is None else 8
+        self._list = (sb_adamw_tensor * n)()
+        self.cfg = sb_adamw_config(seed, bits, SB_DT_F32)
+        for i, (e, p) in enumerate(zip(self._list, params)):
+            k = p.numel()
+            e.n, e.param = k, _dense(f"params[{i}]", p, p.shape, torch.float32, dev)
+            for name, side, scale in (("m", m[i], m_scale), ("v", v[i], v_scale)):
+                dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn if name == "m" and side.dtype == torch.float8_e4m3fn else torch.uint8
+                if side.numel() != k:
+                    raise SBError(1, f"{name}[{i}] has {side.numel()} elements, the parameter {k}")
+                setattr(e, name, _dense(f"{name}[{i}]", side, side.shape, dtype, dev))
+                if bits == 8:
+                    setattr(e, name + "_scale", _dense(f"{name}_scale[{i}]", scale[i], (-(-k // 256),), torch.float32, dev))
+            if shadows is not None:
+                e.shadow = _dense(f"shadows[{i}]", shadows[i], p.shape, torch.bfloat16, dev)
+        self.device = dev
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        torch, params = self._t[:2]
+        dtype = grads[0].dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise SBError(1, f"gradients: float32 or bfloat16, not {dtype}")
+        for i, (e, p, g) in enumerate(zip(self._list, params, grads)):
+            e.grad = _dense(f"grads[{i}]", g, p.shape, dtype, self.device)
+        self.cfg.grad_dtype = SB_DT_BF16 if dtype == torch.bfloat16 else SB_DT_F32
+        self._grads = grads
+
+    def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
+        """dev_step (int64) / dev_lr (float32): one-element device tensors to read instead of step / lr, for a step captured into a graph."""
+        torch, here, stream = _on_device(self._t[1][0])
+        h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _dense("dev_step", dev_step, (1,), torch.int64, self.device),
+                           _dense("dev_lr", dev_lr, (1,), torch.float32, self.device))
+        with here:
+            _check(sb_adamw_tensors(self._list, len(self._list), byref(self.cfg), byref(h), step, stream))
+
+    def moments(self):
+        """What the 8-bit moments stand for: two lists of bf16 tensors."""
+        torch, params = self._t[:2]
+        _, here, stream = _on_device(params[0])
+        with here:
+            out = [[torch.empty(p.shape, dtype=torch.bfloat16, device=self.device) for p in params] for _ in range(2)]
+            ptrs = [(c_void_p * len(params))(*[t.data_ptr() for t in side]) for side in out]
+            _check(sb_adamw_moments(self._list, len(self._list), byref(self.cfg), *ptrs, stream))
+        return out
+
+
+def ops_check(device="cuda"):
+    """Waits for the device's current stream; SBError (SB_ERR_TIMEOUT) if a bounded wait ran out in an operator's kernel."""
+    import torch
+    with torch.cuda.device(device):
+        _check(sb_ops_check(torch.cuda.current_stream().cuda_stream))
 
 
 def _check(status):

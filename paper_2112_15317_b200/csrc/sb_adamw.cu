@@ -1,0 +1,406 @@
+// AdamW over a list of tensors in one kernel, moments in 32 or in 8 bits.
+//
+//   m <- b1 m + (1 - b1) g       v <- b2 v + (1 - b2) g^2
+//   p <- (1 - lr wd) p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)          (and, where wanted, p's bf16 copy)
+//
+// What bounds it: HBM.  A parameter moves 28 bytes with float moments and gradients, 14 with 8-bit moments and bf16 gradients (plus 2 for
+// the bf16 copy).  A warp walks blocks of 256 elements, eight consecutive ones a lane, which is also the block that shares a scale of the
+// 8-bit states: its largest magnitudes are one redux instruction, and nothing crosses the warp otherwise.  The tensors' pointers
+// travel as kernel parameters, so that a call needs no table in device memory and can be captured into a graph as it is.
+//
+// 8-bit moments.  The scale of a block is a power of two, so that scaling rounds nothing and the codes depend on the moments alone.
+//   m: e4m3 of m / (scale = 2^(floor(log2 max) - 7)), to nearest even.  A step moves m by a tenth, more than half a code.
+//   v: five bits of exponent and three of mantissa, no sign, of v / (scale = 2^floor(log2 max)).  A step moves v by a thousandth, which
+//      rounding to nearest would never show: it is rounded up or down by chance, with 16 random bits for each element from
+//      Philox-4x32-10 (counter = {element / 8, tensor, step}, key = seed), so that its expectation is the unrounded value.
+//      Held in the bits of a float: value * 2^-97 has the code in its bits 20 .. 27, subnormal numbers included.
+// A moment that is not finite becomes a code of its own (0x7F, 255) and leaves its block's scale alone.
+// The moments are rounded in the order the formulas above are written in, without fused multiply-adds: with the codes' coarse
+// grids one m in a hundred lies exactly between two codes, and falls to the same side in every implementation that keeps the order.
+#include "../../include/splitbrain.h"
+#include "sb_internal.h"
+
+#include <cuda_fp8.h>
+
+#include <cmath>
+
+namespace sb {
+
+namespace {
+
+constexpr int ADAMW_THREADS = 256, QBLOCK = 256;
+
+struct Entry {
+    float* p;
+    const void* g;
+    void *m, *v;
+    float *ms, *vs;
+    __nv_bfloat16* shadow;
+    int64_t n, first;        // elements; blocks of all tensors before this one
+    int vec, index;          // every pointer suits 16-byte accesses; place in the caller's list
+};
+template <int N> struct AdamwArgs {
+    Entry e[N];
+    int count;
+    int64_t blocks;
+    float b1, c1, b2, c2, decay, rate, rs2, eps;
+    double beta1, beta2, lr, wd;
+    const int64_t* dev_step;
+    const float* dev_lr;
+    uint32_t key0, key1, step;
+};
+
+__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
+{
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0, h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
+        c0 = h1 ^ c1 ^ k0; c1 = l1; c2 = h0 ^ c3 ^ k1; c3 = l0;
+        k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// Eight consecutive elements from i on, n of the tensor in all: 16-byte accesses where the whole run is there and aligned.
+__device__ __forceinline__ void load8(const float* p, int64_t i, int64_t n, bool vec, float (&o)[8])
+{
+    if (vec && i + 8 <= n) {
+        const float4 a = __ldcs((const float4*)(p + i)), b = __ldcs((const float4*)(p + i) + 1);
+        o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w; o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = i + j < n ? p[i + j] : 0.f;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int64_t i, int64_t n, bool vec, float (&o)[8])
+{
+    if (vec && i + 8 <= n) {
+        const uint4 a = __ldcs((const uint4*)(p + i));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { o[2 * j] = __uint_as_float(w[j] << 16); o[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = i + j < n ? __bfloat162float(p[i + j]) : 0.f;
+}
+__device__ __forceinline__ void store8(float* p, int64_t i, int64_t n, bool vec, const float (&v)[8])
+{
+    if (vec && i + 8 <= n) {
+        __stcs((float4*)(p + i), make_float4(v[0], v[1], v[2], v[3]));
+        __stcs((float4*)(p + i) + 1, make_float4(v[4], v[5], v[6], v[7]));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) p[i + j] = v[j];
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int64_t i, int64_t n, bool vec, const float (&v)[8])
+{
+    if (vec && i + 8 <= n) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]); w[j] = *(const uint32_t*)&b; }
+        __stcs((uint4*)(p + i), make_uint4(w[0], w[1], w[2], w[3]));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) p[i + j] = __float2bfloat16_rn(v[j]);
+}
+__device__ __forceinline__ void load_codes(const uint8_t* p, int64_t i, int64_t n, bool vec, uint32_t (&o)[2])
+{
+    if (vec && i + 8 <= n) {
+        const uint2 a = __ldcs((const uint2*)(p + i));
+        o[0] = a.x; o[1] = a.y;
+        return;
+    }
+    o[0] = o[1] = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) o[j / 4] |= (uint32_t)p[i + j] << (8 * (j % 4));
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, bool vec, const uint32_t (&v)[2])
+{
+    if (vec && i + 8 <= n) {
+        __stcs((uint2*)(p + i), make_uint2(v[0], v[1]));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) p[i + j] = (uint8_t)(v[j / 4] >> (8 * (j % 4)));
+}
+
+__device__ __forceinline__ void decode_m(const uint32_t (&c)[2], float scale, float (&o)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[j / 2] >> (16 * (j % 2))), __NV_E4M3);
+        const float2 f = __half22float2(*(const __half2*)&h);
+        o[2 * j] = f.x * scale;
+        o[2 * j + 1] = f.y * scale;
+    }
+}
+__device__ __forceinline__ void decode_v(const uint32_t (&c)[2], float scale, float (&o)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t code = (c[j / 4] >> (8 * (j % 4))) & 255u;
+        o[j] = code == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(code << 20) * 0x1p97f * scale;
+    }
+}
+// The power of two at or below the largest finite magnitude of a warp's block, 2^-100 at least.
+__device__ __forceinline__ float block_power(const float (&a)[8])
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(a[j]) & 0x7fffffffu;
+        if (b < 0x7f800000u && b > top) top = b;
+    }
+    top = __reduce_max_sync(0xffffffffu, top) & 0x7f800000u;
+    return __uint_as_float(top > 0x0d800000u ? top : 0x0d800000u);
+}
+__device__ __forceinline__ void encode_m(const float (&a)[8], float inv, uint32_t (&c)[2])
+{
+    c[0] = c[1] = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(a[2 * j] * inv, a[2 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        if (isinf(a[2 * j])) two |= 0x7fu;           // (the conversion keeps NaN, but takes infinities for the largest number)
+        if (isinf(a[2 * j + 1])) two |= 0x7f00u;
+        c[j / 2] |= two << (16 * (j % 2));
+    }
+}
+__device__ __forceinline__ void encode_v(const float (&a)[8], float inv, uint4 r, uint32_t (&c)[2])
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    c[0] = c[1] = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t half = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu;
+        uint32_t code = (__float_as_uint(a[j] * inv * 0x1p-97f) + (half << 4)) >> 20;
+        code = !isfinite(a[j]) ? 255u : code < 254u ? code : 254u;
+        c[j / 4] |= code << (8 * (j % 4));
+    }
+}
+
+// Warp w's block: the tensor it lies in (binary search over the tensors' first blocks), and its first element there.
+template <int N>
+__device__ __forceinline__ int find_entry(const AdamwArgs<N>& a, int64_t block)
+{
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.e[mid].first <= block) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <int N, int BITS, typename G>
+__global__ void __launch_bounds__(ADAMW_THREADS)
+adamw_kernel(const __grid_constant__ AdamwArgs<N> a)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x % 32;
+    float decay = a.decay, rate = a.rate, rs2 = a.rs2;
+    uint32_t step = a.step;
+    if (a.dev_step != nullptr || a.dev_lr != nullptr) {      // (a replayed step: what changes from replay to replay lies in device memory)
+        __shared__ float s_words[3];
+        __shared__ uint32_t s_step;
+        if (threadIdx.x == 0) {
+            const double lr = a.dev_lr ? (double)*a.dev_lr : a.lr;
+            const int64_t t = a.dev_step ? *a.dev_step : (int64_t)a.step;
+            s_words[0] = (float)(1.0 - lr * a.wd);
+            s_words[1] = (float)(lr / (1.0 - pow(a.beta1, (double)t)));
+            s_words[2] = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+            s_step = (uint32_t)t;
+        }
+        __syncthreads();
+        decay = s_words[0]; rate = s_words[1]; rs2 = s_words[2]; step = s_step;
+    }
+    const int64_t warps = (int64_t)gridDim.x * (ADAMW_THREADS / 32);
+    for (int64_t b = (int64_t)blockIdx.x * (ADAMW_THREADS / 32) + threadIdx.x / 32; b < a.blocks; b += warps) {
+        const Entry& e = a.e[find_entry(a, b)];
+        const int64_t q = b - e.first, i = q * QBLOCK + lane * 8, n = e.n;
+        const bool vec = e.vec != 0;
+        float p[8], g[8], m[8], v[8];
+        load8(e.p, i, n, vec, p);
+        load8((const G*)e.g, i, n, vec, g);
+        if (BITS == 32) {
+            load8((const float*)e.m, i, n, vec, m);
+            load8((const float*)e.v, i, n, vec, v);
+        } else {
+            uint32_t cm[2], cv[2];
+            load_codes((const uint8_t*)e.m, i, n, vec, cm);
+            load_codes((const uint8_t*)e.v, i, n, vec, cv);
+            decode_m(cm, e.ms[q], m);
+            decode_v(cv, e.vs[q], v);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            m[j] = __fadd_rn(__fmul_rn(a.b1, m[j]), __fmul_rn(a.c1, g[j]));
+            v[j] = __fadd_rn(__fmul_rn(a.b2, v[j]), __fmul_rn(__fmul_rn(a.c2, g[j]), g[j]));
+            p[j] = p[j] * decay - rate * m[j] / (sqrtf(v[j]) * rs2 + a.eps);
+        }
+        store8(e.p, i, n, vec, p);
+        if (e.shadow) store8(e.shadow, i, n, vec, p);
+        if (BITS == 32) {
+            store8((float*)e.m, i, n, vec, m);
+            store8((float*)e.v, i, n, vec, v);
+        } else {
+            // (elements behind the tensor's end are zero)
+            const float ms = block_power(m) * 0x1p-7f, vs = block_power(v);
+            uint32_t cm[2], cv[2];
+            encode_m(m, 1.0f / ms, cm);
+            const uint64_t eight = (uint64_t)(i / 8);
+            encode_v(v, 1.0f / vs, philox((uint32_t)eight, (uint32_t)(eight >> 32), (uint32_t)e.index, step, a.key0, a.key1), cv);
+            store_codes((uint8_t*)e.m, i, n, vec, cm);
+            store_codes((uint8_t*)e.v, i, n, vec, cv);
+            __syncwarp();                                    // every lane has read the old scales
+            if (lane == 0) { e.ms[q] = ms; e.vs[q] = vs; }
+        }
+    }
+}
+
+// What the 8-bit moments stand for, as bf16 (a code of four significant bits times a power of two fits).
+template <int N>
+__global__ void __launch_bounds__(ADAMW_THREADS)
+adamw_moments_kernel(const __grid_constant__ AdamwArgs<N> a)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x % 32;
+    const int64_t warps = (int64_t)gridDim.x * (ADAMW_THREADS / 32);
+    for (int64_t b = (int64_t)blockIdx.x * (ADAMW_THREADS / 32) + threadIdx.x / 32; b < a.blocks; b += warps) {
+        const Entry& e = a.e[find_entry(a, b)];
+        const int64_t q = b - e.first, i = q * QBLOCK + lane * 8, n = e.n;
+        const bool vec = e.vec != 0;
+        uint32_t c[2];
+        float f[8];
+        load_codes((const uint8_t*)e.m, i, n, vec, c);
+        decode_m(c, e.ms[q], f);
+        store8((__nv_bfloat16*)e.p, i, n, vec, f);           // (the outputs travel in the places of parameter and copy)
+        load_codes((const uint8_t*)e.v, i, n, vec, c);
+        decode_v(c, e.vs[q], f);
+        store8(e.shadow, i, n, vec, f);
+    }
+}
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+template <int N>
+cudaError_t launch_list(AdamwArgs<N>& a, int bits, bool bf16_grad, bool moments, cudaStream_t st)
+{
+    const int64_t want = (a.blocks + ADAMW_THREADS / 32 - 1) / (ADAMW_THREADS / 32);
+    const dim3 grid((unsigned)(want < 148 * 8 ? want : 148 * 8)), block(ADAMW_THREADS);
+    if (moments) return pdl_launch(adamw_moments_kernel<N>, grid, block, 0, st, a);
+    if (bits == 32) return bf16_grad ? pdl_launch(adamw_kernel<N, 32, __nv_bfloat16>, grid, block, 0, st, a) : pdl_launch(adamw_kernel<N, 32, float>, grid, block, 0, st, a);
+    return bf16_grad ? pdl_launch(adamw_kernel<N, 8, __nv_bfloat16>, grid, block, 0, st, a) : pdl_launch(adamw_kernel<N, 8, float>, grid, block, 0, st, a);
+}
+
+// The list in as many launches as it takes: up to 32 tensors as 2.4 KB of parameters, more as up to 28 KB (350 at a time).
+template <int N, typename Fill>
+sb_status run_list(const sb_adamw_tensor* list, int from, int to, int bits, bool bf16_grad, bool moments, cudaStream_t st, Fill fill)
+{
+    static thread_local AdamwArgs<N> a;
+    a = AdamwArgs<N>{};
+    fill(a);
+    for (int i = from; i < to; ++i) {
+        if (list[i].n == 0) continue;
+        const sb_adamw_tensor& t = list[i];
+        Entry& e = a.e[a.count++];
+        e.p = t.param; e.g = t.grad; e.m = t.m; e.v = t.v; e.ms = t.m_scale; e.vs = t.v_scale; e.shadow = (__nv_bfloat16*)t.shadow;
+        e.n = t.n; e.first = a.blocks; e.index = i;
+        e.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, bits == 32 ? 16 : 8) && aligned(t.v, bits == 32 ? 16 : 8) && aligned(t.shadow, 16);
+        a.blocks += (t.n + QBLOCK - 1) / QBLOCK;
+    }
+    if (a.count == 0) return SB_OK;
+    const cudaError_t e = launch_list(a, bits, bf16_grad, moments, st);
+    return e == cudaSuccess ? SB_OK : set_error(SB_ERR_CUDA, "adamw: %s", cudaGetErrorString(e));
+}
+template <typename F>
+sb_status in_pieces(int n, F piece)
+{
+    for (int from = 0; from < n;) {
+        const int to = n - from <= 32 ? n : n - from < 350 ? n : from + 350;
+        const sb_status s = piece(from, to, to - from <= 32);
+        if (s != SB_OK) return s;
+        from = to;
+    }
+    return SB_OK;
+}
+
+sb_status check_list(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg)
+{
+    if (n < 0 || (n > 0 && !list) || !cfg) return set_error(SB_ERR_INVALID_ARG, "null list or config, or a negative count");
+    if (cfg->state_bits != 32 && cfg->state_bits != 8) return set_error(SB_ERR_INVALID_ARG, "state_bits must be 32 or 8 (got %d)", cfg->state_bits);
+    if (cfg->grad_dtype != SB_DT_F32 && cfg->grad_dtype != SB_DT_BF16) return set_error(SB_ERR_INVALID_ARG, "gradients are SB_DT_F32 or SB_DT_BF16");
+    const size_t ga = cfg->grad_dtype == SB_DT_F32 ? 4 : 2, sa = cfg->state_bits == 32 ? 4 : 1;
+    for (int32_t i = 0; i < n; ++i) {
+        const sb_adamw_tensor& t = list[i];
+        if (t.n < 0) return set_error(SB_ERR_SHAPE, "tensor %d: negative size", i);
+        if (t.n == 0) continue;
+        if (!t.m || !t.v || !aligned(t.m, sa) || !aligned(t.v, sa)) return set_error(SB_ERR_INVALID_ARG, "tensor %d: a moment is null or misaligned", i);
+        if (cfg->state_bits == 8 && (!t.m_scale || !t.v_scale || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4)))
+            return set_error(SB_ERR_INVALID_ARG, "tensor %d: 8-bit moments need their scales", i);
+        if (!t.param || !aligned(t.param, 4)) return set_error(SB_ERR_INVALID_ARG, "tensor %d: the parameter is null or misaligned", i);
+        if (!t.grad || !aligned(t.grad, ga)) return set_error(SB_ERR_INVALID_ARG, "tensor %d: the gradient is null or misaligned", i);
+        if (!aligned(t.shadow, 2)) return set_error(SB_ERR_INVALID_ARG, "tensor %d: the bf16 copy is misaligned", i);
+    }
+    return SB_OK;
+}
+
+}  // namespace
+}  // namespace sb
+
+using namespace sb;
+
+extern "C" {
+
+sb_status sb_adamw_tensors(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, const sb_adamw_hyper* h, int64_t step, void* stream)
+{
+    const sb_status c = check_list(list, n, cfg);
+    if (c != SB_OK) return c;
+    if (!h) return set_error(SB_ERR_INVALID_ARG, "null hyper-parameters");
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0)) return set_error(SB_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+    if (!(h->eps >= 0.0) || !std::isfinite(h->lr) || !std::isfinite(h->weight_decay) || !std::isfinite(h->eps)) return set_error(SB_ERR_INVALID_ARG, "lr, eps and weight_decay must be finite, eps not negative");
+    if (!h->dev_step && step < 1) return set_error(SB_ERR_INVALID_ARG, "the step number starts at 1 (got %lld)", (long long)step);
+    if (!aligned(h->dev_step, 8) || !aligned(h->dev_lr, 4)) return set_error(SB_ERR_INVALID_ARG, "dev_step or dev_lr is misaligned");
+    auto fill = [&](auto& a) {
+        const double t = h->dev_step ? 1.0 : (double)step;
+        a.beta1 = h->beta1; a.beta2 = h->beta2; a.lr = h->lr; a.wd = h->weight_decay;
+        a.b1 = (float)h->beta1; a.c1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.c2 = (float)(1.0 - h->beta2); a.eps = (float)h->eps;
+        a.decay = (float)(1.0 - h->lr * h->weight_decay);
+        a.rate = (float)(h->lr / (1.0 - std::pow(h->beta1, t)));
+        a.rs2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, t)));
+        a.dev_step = h->dev_step; a.dev_lr = h->dev_lr;
+        a.key0 = (uint32_t)cfg->seed; a.key1 = (uint32_t)(cfg->seed >> 32); a.step = (uint32_t)step;
+    };
+    const bool bf = cfg->grad_dtype == SB_DT_BF16;
+    return in_pieces(n, [&](int from, int to, bool few) {
+        return few ? run_list<32>(list, from, to, cfg->state_bits, bf, false, (cudaStream_t)stream, fill)
+                   : run_list<350>(list, from, to, cfg->state_bits, bf, false, (cudaStream_t)stream, fill);
+    });
+}
+
+sb_status sb_adamw_moments(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, void* const* m_out, void* const* v_out, void* stream)
+{
+    const sb_status c = check_list(list, n, cfg);
+    if (c != SB_OK) return c;
+    if (cfg->state_bits != 8) return set_error(SB_ERR_INVALID_ARG, "float moments are what they stand for: read them where they are");
+    if (n > 0 && (!m_out || !v_out)) return set_error(SB_ERR_INVALID_ARG, "null outputs");
+    for (int32_t i = 0; i < n; ++i)
+        if (list[i].n > 0 && (!m_out[i] || !v_out[i] || !aligned(m_out[i], 2) || !aligned(v_out[i], 2)))
+            return set_error(SB_ERR_INVALID_ARG, "tensor %d: an output is null or misaligned", i);
+    auto piece = [&](int from, int to, bool few) {
+        // the outputs in the places of parameter and copy
+        sb_adamw_tensor out[350];
+        for (int i = from; i < to; ++i) { out[i - from] = list[i]; out[i - from].param = (float*)m_out[i]; out[i - from].shadow = v_out[i]; out[i - from].grad = nullptr; }
+        auto fill = [](auto&) {};
+        return few ? run_list<32>(out, 0, to - from, 8, false, true, (cudaStream_t)stream, fill)
+                   : run_list<350>(out, 0, to - from, 8, false, true, (cudaStream_t)stream, fill);
+    };
+    return in_pieces(n, piece);
+}
+
+}  // extern "C"

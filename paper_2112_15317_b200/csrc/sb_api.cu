@@ -33,6 +33,14 @@ static sb_status fail(sb_status s, const char* fmt, ...)
     return s;
 }
 extern "C" const char* sb_last_error(void) { return g_err; }
+sb_status sb::set_error(sb_status s, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return s;
+}
 
 #define CU_TRY(expr)                                                                             \
     do {                                                                                         \

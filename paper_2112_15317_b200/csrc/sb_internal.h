@@ -2,6 +2,7 @@
 // Nothing here is part of the public C ABI (see include/splitbrain.h).
 #pragma once
 
+#include "../../include/splitbrain.h"
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -13,6 +14,9 @@
 namespace sb {
 
 constexpr int MAX_PARTS = 64;  // upper bound on R and K
+
+// Sets the calling thread's message of sb_last_error() and returns `s` (sb_api.cu).
+sb_status set_error(sb_status s, const char* fmt, ...);
 
 // ---------------------------------------------------------------------------------------------
 // Programmatic dependent launch.  Every kernel of the library starts with pdl_prologue(): it waits until the
