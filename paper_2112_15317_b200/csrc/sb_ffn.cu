@@ -7,6 +7,7 @@
 // terms on tensor cores, or CUDA cores; any width) with GU and dH in float between them.  Roundings in bf16: H, and dG and dU, where they become
 // operands of a product; everything else is rounded once, at the end.
 #include "sb_ffn.h"
+#include "sb_ffn_umma.h"
 
 #include <algorithm>
 
@@ -227,7 +228,7 @@ sb_status sb_ffn_bytes(const sb_ffn_config* c, int32_t backward, size_t* bytes)
     const sb_status s = check_config(c);
     if (s != SB_OK) return s;
     if (!bytes) return set_error(SB_ERR_INVALID_ARG, "bytes is null");
-    *bytes = c->rows == 0 ? 0 : ffn_any_bytes(c, backward != 0);
+    *bytes = c->rows == 0 ? 0 : ffn_umma_ok(c) ? ffn_umma_bytes(c, backward != 0) : ffn_any_bytes(c, backward != 0);
     return SB_OK;
 }
 
@@ -261,6 +262,7 @@ sb_status sb_ffn_forward(const sb_ffn_config* c, const void* x, const void* w_ga
     if (!x || !w_gate_up || !w_down || !y) return set_error(SB_ERR_INVALID_ARG, "null matrix");
     if (!aligned16(x) || !aligned16(w_gate_up) || !aligned16(w_down) || !aligned16(gu) || !aligned16(y)) return set_error(SB_ERR_INVALID_ARG, "every matrix must be 16-byte aligned");
     if (!ops_status()) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
+    if (ffn_umma_ok(c)) return ffn_umma_forward(c, x, w_gate_up, w_down, gu, y, ws, (cudaStream_t)stream);
     return any_forward(c, x, w_gate_up, w_down, gu, y, ws, (cudaStream_t)stream);
 }
 
@@ -279,6 +281,7 @@ sb_status sb_ffn_backward(const sb_ffn_config* c, const void* dy, const void* x,
     }
     if (!dy || !x || !gu || !w_gate_up || !w_down) return set_error(SB_ERR_INVALID_ARG, "null matrix");
     if (!ops_status()) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
+    if (ffn_umma_ok(c)) return ffn_umma_backward(c, dy, x, gu, w_gate_up, w_down, dx, dw_gate_up, dw_down, ws, (cudaStream_t)stream);
     return any_backward(c, dy, x, gu, w_gate_up, w_down, dx, dw_gate_up, dw_down, ws, (cudaStream_t)stream);
 }
 

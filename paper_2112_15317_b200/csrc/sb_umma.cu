@@ -1648,58 +1648,6 @@ umma_halo_persist_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_
 //     128..255 in the peer's, same column range) and releases ring slot s in BOTH CTAs with a multicast commit;
 //   * each CTA's epilogue warps read their own TMEM and write their own 128 output rows.
 // No load uses multicast.  All waits are bounded as in the single-CTA kernel.
-__device__ __forceinline__ uint32_t cluster_ctarank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t caddr)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
-    return v;
-}
-// TMA load whose completion may signal a barrier in the peer CTA (`bar_caddr` is a shared::cluster address)
-__device__ __forceinline__ void tma_load_4d_pair_el(const CUtensorMap* map, uint32_t dst_saddr, uint32_t bar_caddr, int c0, int c1, int c2, int c3,
-                                                    uint32_t elected)
-{
-    asm volatile(
-        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %7, 0;\n\t"
-        "@q cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n\t}"
-        ::"r"(dst_saddr), "l"(map), "r"(bar_caddr), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(elected)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst_smem, uint32_t ncols)
-{
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tmem_relinquish_pair()
-{
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols)
-{
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-// arrives (once the MMAs issued so far have completed) on the barrier at this offset in both CTAs of the pair
-__device__ __forceinline__ void umma_commit_pair(uint64_t* bar)
-{
-    const uint16_t mask = 3;
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(smem_u32(bar)), "h"(mask) : "memory");
-}
-
 template <int BN> struct PairCfg {
     static constexpr int B_HALF_BYTES = BN * 64;                       // BN/2 rows (or K x BN/2 columns) of 128 bytes
     static constexpr int STAGE_BYTES = A_STAGE_BYTES + B_HALF_BYTES;
@@ -2331,6 +2279,14 @@ static bool mat_map(CUtensorMap* map, const void* ptr, long rows, long cols, int
 {
     uint64_t d[4] = {(uint64_t)cols, (uint64_t)rows, 1, 1};
     uint64_t s[3] = {(uint64_t)cols * 2, (uint64_t)rows * cols * 2, (uint64_t)rows * cols * 2};
+    uint32_t b[4] = {64, (uint32_t)box_rows, 1, 1};
+    return encode_map(map, ptr, d, s, b);
+}
+
+bool umma_map_rows(CUtensorMap* map, const void* ptr, long rows, long cols, long ld, int box_rows)
+{
+    uint64_t d[4] = {(uint64_t)cols, (uint64_t)rows, 1, 1};
+    uint64_t s[3] = {(uint64_t)ld * 2, (uint64_t)ld * 2, (uint64_t)ld * 2};      // (the outer dimensions are one)
     uint32_t b[4] = {64, (uint32_t)box_rows, 1, 1};
     return encode_map(map, ptr, d, s, b);
 }
