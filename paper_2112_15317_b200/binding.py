@@ -8,7 +8,9 @@ importing this module without the built library raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
@@ -247,22 +249,23 @@ def conv_in_wgrad_static(x, dy, dw, db, precision):
 # Dense CUDA tensors of one device; outputs and workspaces come from torch's allocator, on the current stream of that device.
 
 
+_here = contextlib.nullcontext()
+
+
 def _on_device(t):
     """(torch, the tensor's device as a context where it is not the current one, its current stream as a pointer)"""
-    import contextlib
     import torch
-    d = t.device
-    if d.type != "cuda":
-        raise SBError(1, f"the tensors must lie on a CUDA device (got {d})")
-    here = contextlib.nullcontext() if d.index == torch.cuda.current_device() else torch.cuda.device(d)
-    return torch, here, torch._C._cuda_getCurrentRawStream(d.index)
+    d = t.get_device()
+    if d < 0:
+        raise SBError(1, f"the tensors must lie on a CUDA device (got {t.device})")
+    return torch, _here if d == torch._C._cuda_getDevice() else torch.cuda.device(d), torch._C._cuda_getCurrentRawStream(d)
 
 
 def _dense(name, t, shape, dtype, device):
     """The tensor's address; SBError if it is not what the call needs."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise SBError(1, f"{name}: expected a dense {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)}"
                          f" {'' if t.is_contiguous() else 'with strides ' + str(t.stride()) + ' '}on {t.device}")
     return t.data_ptr()
@@ -276,33 +279,38 @@ def _precision(torch, t):
     raise SBError(1, f"x: float32 or bfloat16, not {t.dtype}")
 
 
-def _workspace(torch, nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
-def _ffn_config(torch, x, w_gate_up, w_down, act, grad_dtype=SB_DT_F32):
+# (a call's sizes fix its configuration and its workspace: looked up once per set of sizes)
+@functools.lru_cache(maxsize=1024)
+def _ffn_config(rows, d, f, act, precision, grad_dtype, backward):
+    c, n = sb_ffn_config(rows, d, f, act, precision, grad_dtype), c_size_t()
+    _check(sb_ffn_bytes(byref(c), backward, byref(n)))
+    return byref(c), n.value
+
+
+def _ffn_call(torch, x, w_gate_up, w_down, act, backward, grad_dtype=SB_DT_F32):
     if x.dim() != 2 or w_gate_up.dim() != 2:
         raise SBError(2, "x and w_gate_up must be matrices")
     rows, d = x.shape
     f = w_gate_up.shape[0] // 2
-    _dense("x", x, (rows, d), x.dtype, x.device)
-    c = sb_ffn_config(rows, d, f, act, _precision(torch, x), grad_dtype)
-    return c, _dense("w_gate_up", w_gate_up, (2 * f, d), x.dtype, x.device), _dense("w_down", w_down, (d, f), x.dtype, x.device)
+    dtype, device = x.dtype, x.device
+    ptrs = _dense("x", x, x.shape, dtype, device), _dense("w_gate_up", w_gate_up, (2 * f, d), dtype, device), _dense("w_down", w_down, (d, f), dtype, device)
+    return (rows, f, *_ffn_config(rows, d, f, act, _precision(torch, x), grad_dtype, backward), *ptrs)
 
 
 def ffn_forward(x, w_gate_up, w_down, act=SB_ACT_SILU, save=False):
     """Gated feed-forward block: (a(x Wg^T) * (x Wu^T)) Wd^T with w_gate_up = [Wg; Wu].  x [rows, d], w_gate_up [2f, d], w_down [d, f].
     save: returns (y, gu), gu [rows, 2f] being what ffn_backward needs."""
     torch, here, stream = _on_device(x)
-    c, wgu, wd = _ffn_config(torch, x, w_gate_up, w_down, act)
+    rows, f, c, n, px, pgu, pd = _ffn_call(torch, x, w_gate_up, w_down, act, 0)
     with here:
-        n = c_size_t()
-        _check(sb_ffn_bytes(byref(c), 0, byref(n)))
-        ws = _workspace(torch, n.value, x.device)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
         y = torch.empty_like(x)
-        gu = torch.empty((c.rows, 2 * c.f), dtype=x.dtype, device=x.device) if save else None
-        _check(sb_ffn_forward(byref(c), x.data_ptr(), wgu, wd, gu.data_ptr() if save else None, y.data_ptr(),
-                              ws.data_ptr() if n.value else None, n.value, stream))
+        gu = torch.empty((rows, 2 * f), dtype=x.dtype, device=x.device) if save else None
+        _check(sb_ffn_forward(c, px, pgu, pd, _address(gu), y.data_ptr(), ws.data_ptr(), n, stream))
     return (y, gu) if save else y
 
 
@@ -313,28 +321,32 @@ def ffn_backward(dy, x, gu, w_gate_up, w_down, act=SB_ACT_SILU, grad_dtype=None,
     grad_dtype = x.dtype if grad_dtype is None else grad_dtype
     if grad_dtype not in (torch.float32, torch.bfloat16):
         raise SBError(1, f"grad_dtype: float32 or bfloat16, not {grad_dtype}")
-    c, wgu, wd = _ffn_config(torch, x, w_gate_up, w_down, act, SB_DT_BF16 if grad_dtype == torch.bfloat16 else SB_DT_F32)
-    pdy, pgu = _dense("dy", dy, x.shape, x.dtype, x.device), _dense("gu", gu, (c.rows, 2 * c.f), x.dtype, x.device)
+    rows, f, c, n, px, pgu, pd = _ffn_call(torch, x, w_gate_up, w_down, act, 1, SB_DT_BF16 if grad_dtype == torch.bfloat16 else SB_DT_F32)
+    pdy, pkept = _dense("dy", dy, x.shape, x.dtype, x.device), _dense("gu", gu, (rows, 2 * f), x.dtype, x.device)
     with here:
-        n = c_size_t()
-        _check(sb_ffn_bytes(byref(c), 1, byref(n)))
-        ws = _workspace(torch, n.value, x.device)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
         dx = torch.empty_like(x) if needs[0] else None
         dwgu = torch.empty(w_gate_up.shape, dtype=grad_dtype, device=x.device) if needs[1] else None
         dwd = torch.empty(w_down.shape, dtype=grad_dtype, device=x.device) if needs[2] else None
-        _check(sb_ffn_backward(byref(c), pdy, x.data_ptr(), pgu, wgu, wd, *[None if t is None else t.data_ptr() for t in (dx, dwgu, dwd)],
-                               ws.data_ptr() if n.value else None, n.value, stream))
+        _check(sb_ffn_backward(c, pdy, px, pkept, pgu, pd, _address(dx), _address(dwgu), _address(dwd), ws.data_ptr(), n, stream))
     return dx, dwgu, dwd
 
 
-def _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, eps):
+@functools.lru_cache(maxsize=1024)
+def _norm_config(rows, groups, d, kind, precision, eps):
+    c, n = sb_norm_config(rows, groups, d, kind, precision, eps), c_size_t()
+    _check(sb_norm_bytes(byref(c), byref(n)))
+    return byref(c), n.value
+
+
+def _norm_call(torch, x, w_pre, f, w_post, gate, scale, kind, eps):
     if x.dim() != 2 or (gate is not None and gate.dim() != 2):
         raise SBError(2, "x and gate must be matrices")
     rows, d = x.shape
-    f32, dev = torch.float32, x.device
-    c = sb_norm_config(rows, 0 if gate is None else gate.shape[0], d, kind, _precision(torch, x), eps)
-    return c, [_dense("x", x, (rows, d), x.dtype, dev), _dense("w_pre", w_pre, (d,), f32, dev), _dense("f", f, (rows, d), x.dtype, dev),
-               _dense("w_post", w_post, (d,), f32, dev), _dense("gate", gate, (c.groups, d), f32, dev), _dense("scale", scale, (d,), f32, dev)]
+    f32, dev, groups = torch.float32, x.device, 0 if gate is None else gate.shape[0]
+    ptrs = [_dense("x", x, x.shape, x.dtype, dev), _dense("w_pre", w_pre, (d,), f32, dev), _dense("f", f, x.shape, x.dtype, dev),
+            _dense("w_post", w_post, (d,), f32, dev), _dense("gate", gate, (groups, d), f32, dev), _dense("scale", scale, (d,), f32, dev)]
+    return (rows, *_norm_config(rows, groups, d, kind, _precision(torch, x), eps), ptrs)
 
 
 def norm_forward(x, w_pre=None, f=None, w_post=None, gate=None, scale=None, kind=SB_NORM_RMS, eps=1e-6, save=False):
@@ -342,13 +354,13 @@ def norm_forward(x, w_pre=None, f=None, w_post=None, gate=None, scale=None, kind
     gate ([groups, d], a row for rows / groups rows of x) and the residual scale.  Without f, y is x; without w_pre there is no n.
     Returns (y, n), and with save (y, n, stats) for norm_backward."""
     torch, here, stream = _on_device(x)
-    c, ptrs = _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, eps)
+    rows, c, _, ptrs = _norm_call(torch, x, w_pre, f, w_post, gate, scale, kind, eps)
     with here:
-        y = x if f is None else torch.empty_like(x)
+        y = None if f is None else torch.empty_like(x)
         n = torch.empty_like(x) if w_pre is not None else None
-        stats = torch.empty((c.rows, 4), dtype=torch.float32, device=x.device) if save else None
-        _check(sb_norm_forward(byref(c), *ptrs, None if f is None else y.data_ptr(), None if n is None else n.data_ptr(),
-                               stats.data_ptr() if save else None, stream))
+        stats = torch.empty((rows, 4), dtype=torch.float32, device=x.device) if save else None
+        _check(sb_norm_forward(c, *ptrs, _address(y), _address(n), _address(stats), stream))
+    y = x if f is None else y
     return (y, n, stats) if save else (y, n)
 
 
@@ -356,20 +368,15 @@ def norm_backward(dy, dn, stats, x, w_pre=None, f=None, w_post=None, gate=None, 
     """Gradients of norm_forward from those of y and n (either may be None) as a dict: dx, df, dw_pre, dw_post, dgate, dscale (None where there
     is no such input; dw_pre also without dn)."""
     torch, here, stream = _on_device(x)
-    c, ptrs = _norm_config(torch, x, w_pre, f, w_post, gate, scale, kind, 0.0)
+    rows, c, n, ptrs = _norm_call(torch, x, w_pre, f, w_post, gate, scale, kind, 0.0)
     dev = x.device
     pdy, pdn = _dense("dy", dy, x.shape, x.dtype, dev), _dense("dn", dn, x.shape, x.dtype, dev)
-    pst = _dense("stats", stats, (c.rows, 4), torch.float32, dev)
+    pst = _dense("stats", stats, (rows, 4), torch.float32, dev)
     with here:
-        n = c_size_t()
-        _check(sb_norm_bytes(byref(c), byref(n)))
-        ws = _workspace(torch, n.value, dev)
-        out = {"dx": torch.empty_like(x), "df": None if f is None else torch.empty_like(f), "dw_pre": None if dn is None or w_pre is None else torch.empty_like(w_pre),
-               "dw_post": None if w_post is None else torch.empty_like(w_post), "dgate": None if gate is None else torch.empty_like(gate),
-               "dscale": None if scale is None else torch.empty_like(scale)}
-        _check(sb_norm_backward(byref(c), pdy, pdn, pst, *ptrs, *[None if t is None else t.data_ptr() for t in out.values()],
-                                ws.data_ptr() if n.value else None, n.value, stream))
-    return out
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        out = [None if t is None else torch.empty_like(t) for t in (x, f, w_pre if dn is not None else None, w_post, gate, scale)]
+        _check(sb_norm_backward(c, pdy, pdn, pst, *ptrs, *map(_address, out), ws.data_ptr(), n, stream))
+    return dict(zip(("dx", "df", "dw_pre", "dw_post", "dgate", "dscale"), out))
 
 
 class AdamW:

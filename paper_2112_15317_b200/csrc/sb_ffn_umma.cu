@@ -9,7 +9,7 @@
 //
 // Operands are K-major or MN-major as they lie in memory (nothing is transposed): the shared-memory descriptors and the instruction descriptor say
 // which, per problem.  A stage of the ring is 64 reduction steps: 128 x 64 of A and, since the MMA of a pair reads both CTAs' halves, 128 x 64 of B in
-// each CTA.  Warps: 0 = TMA loads, 1 = TMEM and (leader) MMA, 2 .. 9 = epilogue, two groups of four warps, each with half of the columns; two
+// each CTA.  Warps: 0 = TMA loads, 1 = TMEM and (leader) MMA, 2 .. 17 = epilogue, two groups of eight warps, each with half of the columns; two
 // accumulators of 256 columns, so that a tile's epilogue runs beside the next tile's MMAs.  Epilogues stage 64-column pieces in the 128-byte swizzle and
 // leave them to TMA stores, which also cut off what lies outside of the matrix.
 //
@@ -25,7 +25,7 @@ namespace sb {
 
 namespace {
 
-constexpr int PT_THREADS = 64 + 256, PT_STAGE = 32768, PT_BOX = 16384, PT_CTRL = 1024, PT_MAX_STAGES = 6;
+constexpr int PT_THREADS = 64 + 512, PT_STAGE = 32768, PT_BOX = 16384, PT_CTRL = 1024, PT_MAX_STAGES = 6;
 constexpr uint32_t PT_TMEM = 512;
 constexpr int PT_SMEM_LIMIT = 227 * 1024;
 enum { EPI_STORE = 0, EPI_GLU = 1, EPI_GLU_BACK = 2 };
@@ -48,7 +48,8 @@ struct alignas(64) PairArgs {
     // Units of the first problem go round the pairs; of its last, incomplete round the pairs without a unit take `extra` units of the other problems
     // each before these go round in turn (dX's reductions are several times as long as those of the weight gradients).
     int pairs, first, rest, odd, extra;
-    int act, save;
+    int save;
+    int stages, slots;                 // EPI_STORE
     uint32_t* status;
 };
 
@@ -100,15 +101,17 @@ __device__ __forceinline__ void stage_bf16(uint32_t box, int r, int c, const flo
     st_shared16(piece(box, r, c + 1), pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]), pack2(v[14], v[15]));
 }
 
-template <int EPI>
+template <int EPI, int ACT>
 __global__ void __launch_bounds__(PT_THREADS, 1)
 ffn_pair_kernel(const __grid_constant__ PairArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    constexpr int ST = pair_stages(EPI), BOXES = group_boxes(EPI);
+    constexpr int BOXES = group_boxes(EPI);
+    // (a fifth of the shared memory is a second set of staging boxes where tiles are short, else two more stages)
+    const int ST = EPI == EPI_STORE ? a.stages : pair_stages(EPI), SLOTS = EPI == EPI_STORE ? a.slots : 1;
     uint8_t* stage_out = smem + ST * PT_STAGE;
-    uint8_t* ctrl = stage_out + 2 * BOXES * PT_BOX;
+    uint8_t* ctrl = smem + pair_stages(EPI) * PT_STAGE + 2 * BOXES * PT_BOX;
     uint64_t* full = (uint64_t*)ctrl;                 // [ST]
     uint64_t* empty = full + PT_MAX_STAGES;           // [ST]
     uint64_t* acc_full = empty + PT_MAX_STAGES;       // [2]
@@ -222,9 +225,13 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
         }
     } else {
         // ---- epilogue: own 128 rows, half of the columns a group ----
-        const int quad = warp % 4, group = (warp - 2) / 4, row = quad * 32 + lane, t128 = (threadIdx.x - 64) % 128;
-        auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); };
-        const uint32_t acc_empty_l = map_to_cta(smem_u32(acc_empty), 0), box0 = smem_u32(stage_out) + (uint32_t)(group * BOXES * PT_BOX);
+        // (two warps of a group share a TMEM lane quadrant: `side` says which columns of a 64-column piece are this one's)
+        const int quad = warp % 4, group = (warp - 2) / 8, side = (warp - 2) / 4 % 2, row = quad * 32 + lane;
+        const bool first = (threadIdx.x - 64) % 256 == 0;
+        auto group_sync = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1 + group) : "memory"); };
+        const uint32_t acc_empty_l = map_to_cta(smem_u32(acc_empty), 0), boxes = smem_u32(stage_out) + (uint32_t)(group * SLOTS * BOXES * PT_BOX);
+        uint32_t box0 = boxes;
+        int slot = 0;
         const uint32_t kept_bar = smem_u32(&kept[group]);
         uint32_t kept_ph = 0u;
         bool ok = true;
@@ -246,7 +253,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
             const int buf = i & 1, m0 = mt * 256 + (int)rank * 128;
             const uint32_t acc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * 256);
             const bool rows_in = m0 < p.m;
-            if (EPI == EPI_GLU_BACK && t128 == 0) {           // the first 64 columns' G and U, into the pieces that their gradients will replace
+            if (EPI == EPI_GLU_BACK && first) {           // the first 64 columns' G and U, into the pieces that their gradients will replace
                 tma_store_wait_read();
                 mbar_arrive_expect_tx(kept_bar, 2u * PT_BOX);
                 tma_load_4d_el(&a.g, box0, kept_bar, nt * 256 + group * 128, m0, 0, 0, 1u);
@@ -254,13 +261,16 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
             }
             if (lane == 0) ok = mbar_wait(&acc_full[buf], (uint32_t)((i >> 1) & 1));
             ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-            if (EPI != EPI_GLU_BACK && t128 == 0) tma_store_wait_read();       // the last tile has left the staging boxes
+            // the tile that was in these staging boxes has left them
+            auto boxes_free = [&]() { if (SLOTS > 1) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); else tma_store_wait_read(); };
+            auto next_boxes = [&]() { if (SLOTS > 1) { slot ^= 1; box0 = boxes + (uint32_t)(slot * BOXES * PT_BOX); } };
+            if (EPI != EPI_GLU_BACK && first) boxes_free();
             if (!agree()) break;
             tc_fence_after();
             if (EPI == EPI_GLU) {
                 const int n0 = nt * 128 + group * 64;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 2 * side; c < 2 * side + 2; ++c) {
                     uint32_t gv[16], uv[16];
                     tmem_ld16(acc + (uint32_t)(group * 64 + c * 16), gv);
                     tmem_ld16(acc + (uint32_t)(128 + group * 64 + c * 16), uv);
@@ -269,7 +279,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         g[j] = __uint_as_float(gv[j]); up[j] = __uint_as_float(uv[j]);
-                        h[j] = ffn_act<false>(g[j], a.act) * up[j];
+                        h[j] = ffn_act<false>(g[j], ACT) * up[j];
                     }
                     stage_bf16(box0, row, 2 * c, h);
                     if (a.save) { stage_bf16(box0 + PT_BOX, row, 2 * c, g); stage_bf16(box0 + 2 * PT_BOX, row, 2 * c, up); }
@@ -277,7 +287,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 tc_fence_before();
                 group_sync();
-                if (t128 == 0) {
+                if (first) {
                     drained(buf);
                     if (rows_in && n0 < p.n)
                         for (int b = 0; b < (a.save ? 3 : 1); ++b) tma_store_4d(&a.c[b], box0 + (uint32_t)(b * PT_BOX), n0, m0, 0, 0);
@@ -287,7 +297,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                 for (int half = 0; half < 2; ++half) {
                     const int n0 = nt * 256 + group * 128 + half * 64;
                     if (half == 1) {
-                        if (t128 == 0) {
+                        if (first) {
                             tma_store_wait_read();
                             mbar_arrive_expect_tx(kept_bar, 2u * PT_BOX);
                             tma_load_4d_el(&a.g, box0, kept_bar, n0, m0, 0, 0, 1u);
@@ -299,7 +309,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                     kept_ph ^= 1u;
                     if (!agree()) break;
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 2 * side; c < 2 * side + 2; ++c) {
                         uint32_t dv[16], gw[8], uw[8];
                         tmem_ld16(acc + (uint32_t)(group * 128 + half * 64 + c * 16), dv);
                         ld_shared16(piece(box0, row, 2 * c), *(uint32_t(*)[4])&gw[0]);
@@ -313,7 +323,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                             const uint32_t gb = j % 2 ? gw[j / 2] & 0xffff0000u : gw[j / 2] << 16, ub = j % 2 ? uw[j / 2] & 0xffff0000u : uw[j / 2] << 16;
                             const float up = __uint_as_float(ub), dh = __uint_as_float(dv[j]);
                             float da;
-                            const float act = ffn_act_grad<false>(__uint_as_float(gb), a.act, da);
+                            const float act = ffn_act_grad<false>(__uint_as_float(gb), ACT, da);
                             dg[j] = dh * up * da;
                             du[j] = dh * act;
                             h[j] = act * up;
@@ -325,7 +335,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tc_fence_before();
                     group_sync();
-                    if (t128 == 0) {
+                    if (first) {
                         if (half == 1) drained(buf);
                         if (rows_in && n0 < p.n)
 #pragma unroll
@@ -338,7 +348,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                 const int n0 = nt * 256 + group * 128;
                 if (!p.out_f32) {
 #pragma unroll 1
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 4 * side; c < 4 * side + 4; ++c) {
                         uint32_t v[16];
                         tmem_ld16(acc + (uint32_t)(group * 128 + c * 16), v);
                         tmem_ld_wait();
@@ -350,20 +360,21 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tc_fence_before();
                     group_sync();
-                    if (t128 == 0) {
+                    if (first) {
                         drained(buf);
                         for (int b = 0; b < 2; ++b)
                             if (rows_in && n0 + 64 * b < p.n) tma_store_4d(&a.c[k], box0 + (uint32_t)(b * PT_BOX), n0 + 64 * b, m0, 0, 0);
                         tma_store_commit();
                     }
+                    next_boxes();
                 } else {
                     for (int half = 0; half < 2; ++half) {       // 64 columns at a time, boxes of 32
                         if (half == 1) {
-                            if (t128 == 0) tma_store_wait_read();
+                            if (first) boxes_free();
                             group_sync();
                         }
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
+                        for (int c = 2 * side; c < 2 * side + 2; ++c) {
                             uint32_t v[16];
                             tmem_ld16(acc + (uint32_t)(group * 128 + half * 64 + c * 16), v);
                             tmem_ld_wait();
@@ -374,17 +385,18 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         tc_fence_before();
                         group_sync();
-                        if (t128 == 0) {
+                        if (first) {
                             if (half == 1) drained(buf);
                             for (int b = 0; b < 2; ++b)
                                 if (rows_in && n0 + 64 * half + 32 * b < p.n) tma_store_4d(&a.c[k], box0 + (uint32_t)(b * PT_BOX), n0 + 64 * half + 32 * b, m0, 0, 0);
                             tma_store_commit();
                         }
+                        next_boxes();
                     }
                 }
             }
         }
-        if (t128 == 0) tma_store_wait_read();
+        if (first) tma_store_wait_read();
     }
 
     // ---- teardown: everyone meets here; TMEM is released on every path ----
@@ -404,7 +416,7 @@ ffn_pair_kernel(const __grid_constant__ PairArgs a)
 
 int cdiv(int64_t x, int64_t y) { return (int)((x + y - 1) / y); }
 
-template <int EPI>
+template <int EPI, int ACT>
 cudaError_t launch_pair(PairArgs& a, cudaStream_t st)
 {
     a.first = a.p[0].units;
@@ -416,8 +428,14 @@ cudaError_t launch_pair(PairArgs& a, cudaStream_t st)
     a.odd = a.first % a.pairs;
     a.extra = 0;
     if (a.rest > 0 && a.odd > 0) a.extra = std::min((a.p[0].chunks + a.p[1].chunks / 2) / std::max(1, a.p[1].chunks), a.rest / (a.pairs - a.odd));
+    // short tiles: their time is the epilogue's, which two sets of staging boxes let run on (weight gradients of 4096 x 8192 over 16 rows: 68 us with one
+    // set, 60 with two; of 2048 x 2048 over 512 rows, eight chunks: 16.3 and 18)
+    int longest = 0;
+    for (int k = 0; k < a.count; ++k) longest = std::max(longest, a.p[k].chunks);
+    a.slots = longest <= 4 ? 2 : 1;
+    a.stages = a.slots == 2 ? 3 : 5;
     a.status = ops_status();
-    const cudaError_t e = raise_smem_limit<ffn_pair_kernel<EPI>>(pair_smem(EPI));
+    const cudaError_t e = raise_smem_limit<ffn_pair_kernel<EPI, ACT>>(pair_smem(EPI));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2 * a.pairs);
@@ -431,7 +449,13 @@ cudaError_t launch_pair(PairArgs& a, cudaStream_t st)
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, ffn_pair_kernel<EPI>, a);
+    return cudaLaunchKernelEx(&cfg, ffn_pair_kernel<EPI, ACT>, a);
+}
+
+template <int EPI>
+cudaError_t launch_pair_act(PairArgs& a, int act, cudaStream_t st)
+{
+    return act == SB_ACT_SILU ? launch_pair<EPI, SB_ACT_SILU>(a, st) : act == SB_ACT_GELU ? launch_pair<EPI, SB_ACT_GELU>(a, st) : launch_pair<EPI, SB_ACT_RELU>(a, st);
 }
 
 // An operand [rows, cols] (rows ld apart): the reduction runs along its rows' columns (mn = 0: boxes of 128 rows) or down its rows (mn = 1: of 64).
@@ -451,6 +475,19 @@ sb_status launched(cudaError_t e) { return e == cudaSuccess ? SB_OK : set_error(
 
 }  // namespace
 
+// Which products run on sb_ffn_rows.cu: those whose estimate there is the shorter one.  Here: 6 us of launch, set-up and the last tile's epilogue (10 with
+// the derivative), 0.33 us a chunk and 2 us (5) of epilogue that hides nothing for each round of tiles over the pairs.
+// (4096 x 8192, forward: 256 rows 62.6 us there and 79.8 here, 512 rows 115 and 101; 1024 x 4096, 512 rows: 27.6 and 35.5, 1024 rows: 42.4 and 41.3.)
+static bool on_rows(int64_t rows, int row_tiles, int mn, const PairProblem& p, bool back)
+{
+#ifdef SB_DEV_TUNING
+    const int force = (int)tune("SB_FEW_ROWS", -1);
+    if (force >= 0) return rows <= force;
+#endif
+    const double here = (back ? 10.0 : 6.0) + cdiv(p.units, 74) * (0.33 * p.chunks + (back ? 5.0 : 2.0));
+    return ffn_rows_us(rows, row_tiles, p.chunks, mn) < here;
+}
+
 bool ffn_umma_ok(const sb_ffn_config* c) { return c->precision == SB_BF16 && c->d % 8 == 0 && c->f % 8 == 0; }
 
 size_t ffn_umma_bytes(const sb_ffn_config* c, bool backward) { return backward ? 3 * h_bytes(c) : h_bytes(c); }
@@ -458,23 +495,29 @@ size_t ffn_umma_bytes(const sb_ffn_config* c, bool backward) { return backward ?
 sb_status ffn_umma_forward(const sb_ffn_config* c, const void* x, const void* w_gu, const void* w_down, void* gu, void* y, void* ws, cudaStream_t st)
 {
     const int64_t R = c->rows, D = c->d, F = c->f;
+    __nv_bfloat16* h = (__nv_bfloat16*)ws;
     static thread_local PairArgs a;
     a = PairArgs{};
-    a.count = 1; a.act = c->act; a.save = gu != nullptr;
+    a.count = 1; a.save = gu != nullptr;
     a.p[0] = problem(R, F, D, 0, 0);
     a.p[0].b_split = (int)F;
     a.p[0].n_tiles = cdiv(F, 128);
     a.p[0].units = a.p[0].m_tiles * a.p[0].n_tiles;
-    bool ok = operand(&a.a[0], x, R, D, 0) && operand(&a.b[0], w_gu, 2 * F, D, 0) && umma_map_rows(&a.c[0], ws, (long)R, (long)F, (long)F, 128);
-    if (ok && gu) ok = umma_map_rows(&a.c[1], gu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[2], (const __nv_bfloat16*)gu + F, (long)R, (long)F, (long)(2 * F), 128);
-    if (!ok) return map_failed();
-    sb_status s = launched(launch_pair<EPI_GLU>(a, st));
+    sb_status s = SB_OK;
+    if (on_rows(R, cdiv(F, 64), 0, a.p[0], false)) s = ffn_rows_glu(c, x, w_gu, gu, h, st);
+    else {
+        bool ok = operand(&a.a[0], x, R, D, 0) && operand(&a.b[0], w_gu, 2 * F, D, 0) && umma_map_rows(&a.c[0], h, (long)R, (long)F, (long)F, 128);
+        if (ok && gu) ok = umma_map_rows(&a.c[1], gu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[2], (const __nv_bfloat16*)gu + F, (long)R, (long)F, (long)(2 * F), 128);
+        if (!ok) return map_failed();
+        s = launched(launch_pair_act<EPI_GLU>(a, c->act, st));
+    }
     if (s != SB_OK) return s;
     a = PairArgs{};
     a.count = 1;
     a.p[0] = problem(R, D, F, 0, 0);
-    if (!operand(&a.a[0], ws, R, F, 0) || !operand(&a.b[0], w_down, D, F, 0) || !umma_map_rows(&a.c[0], y, (long)R, (long)D, (long)D, 128)) return map_failed();
-    return launched(launch_pair<EPI_STORE>(a, st));
+    if (on_rows(R, cdiv(D, 128), 0, a.p[0], false)) return ffn_rows_down(c, h, w_down, y, st);
+    if (!operand(&a.a[0], h, R, F, 0) || !operand(&a.b[0], w_down, D, F, 0) || !umma_map_rows(&a.c[0], y, (long)R, (long)D, (long)D, 128)) return map_failed();
+    return launched(launch_pair<EPI_STORE, 0>(a, st));
 }
 
 sb_status ffn_umma_backward(const sb_ffn_config* c, const void* dy, const void* x, const void* gu, const void* w_gu, const void* w_down, void* dx, void* dw_gu,
@@ -483,24 +526,30 @@ sb_status ffn_umma_backward(const sb_ffn_config* c, const void* dy, const void* 
     const int64_t R = c->rows, D = c->d, F = c->f;
     __nv_bfloat16* h = (__nv_bfloat16*)ws;
     __nv_bfloat16* dgu = (__nv_bfloat16*)((char*)ws + h_bytes(c));
+    const __nv_bfloat16* kept = (const __nv_bfloat16*)gu;
     static thread_local PairArgs a;
     a = PairArgs{};
-    a.count = 1; a.act = c->act;
+    a.count = 1;
     a.p[0] = problem(R, F, D, 0, 1);
-    bool ok = operand(&a.a[0], dy, R, D, 0) && operand(&a.b[0], w_down, D, F, 1);
-    const __nv_bfloat16* kept = (const __nv_bfloat16*)gu;
-    ok = ok && umma_map_rows(&a.g, kept, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.u, kept + F, (long)R, (long)F, (long)(2 * F), 128);
-    ok = ok && umma_map_rows(&a.c[0], dgu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[1], dgu + F, (long)R, (long)F, (long)(2 * F), 128) &&
-         umma_map_rows(&a.c[2], h, (long)R, (long)F, (long)F, 128);
-    if (!ok) return map_failed();
-    sb_status s = launched(launch_pair<EPI_GLU_BACK>(a, st));
+    sb_status s = SB_OK;
+    if (on_rows(R, cdiv(F, 128), 1, a.p[0], true)) s = ffn_rows_glu_back(c, dy, gu, w_down, dgu, h, st);
+    else {
+        bool ok = operand(&a.a[0], dy, R, D, 0) && operand(&a.b[0], w_down, D, F, 1);
+        ok = ok && umma_map_rows(&a.g, kept, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.u, kept + F, (long)R, (long)F, (long)(2 * F), 128);
+        ok = ok && umma_map_rows(&a.c[0], dgu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[1], dgu + F, (long)R, (long)F, (long)(2 * F), 128) &&
+             umma_map_rows(&a.c[2], h, (long)R, (long)F, (long)F, 128);
+        if (!ok) return map_failed();
+        s = launched(launch_pair_act<EPI_GLU_BACK>(a, c->act, st));
+    }
     if (s != SB_OK) return s;
+    const bool dx_rows = dx && on_rows(R, cdiv(D, 128), 1, problem(R, D, 2 * F, 0, 1), false);
+    if (dx_rows && (s = ffn_rows_dx(c, dgu, w_gu, dx, st)) != SB_OK) return s;
     a = PairArgs{};
     const bool f32 = c->grad_dtype == SB_DT_F32;
     auto out = [&](CUtensorMap* map, void* p, int64_t rows, int64_t cols) {
         return f32 ? umma_map_f32_rows(map, p, (long)rows, (long)cols, 128) : umma_map_rows(map, p, (long)rows, (long)cols, (long)cols, 128);
     };
-    if (dx) {
+    if (dx && !dx_rows) {
         const int k = a.count++;
         a.p[k] = problem(R, D, 2 * F, 0, 1);
         if (!operand(&a.a[k], dgu, R, 2 * F, 0) || !operand(&a.b[k], w_gu, 2 * F, D, 1) || !umma_map_rows(&a.c[k], dx, (long)R, (long)D, (long)D, 128)) return map_failed();
@@ -517,7 +566,7 @@ sb_status ffn_umma_backward(const sb_ffn_config* c, const void* dy, const void* 
         a.p[k].out_f32 = f32;
         if (!operand(&a.a[k], dy, R, D, 1) || !operand(&a.b[k], h, R, F, 1) || !out(&a.c[k], dw_down, D, F)) return map_failed();
     }
-    return a.count ? launched(launch_pair<EPI_STORE>(a, st)) : SB_OK;
+    return a.count ? launched(launch_pair<EPI_STORE, 0>(a, st)) : SB_OK;
 }
 
 }  // namespace sb
