@@ -522,7 +522,7 @@ sb_status sb_norm_backward(const sb_norm_config* cfg, const void* dy, const void
  *   at counter {e / 8 (two words), index in the list, step}, key = seed.  Codes 0x7F and 255: not a number.  Zero bytes are zero moments.
  * step: number of this step, from 1.  For a step replayed in a graph: dev_step (int64) and dev_lr (float), DEVICE words that are read
  * instead of `step` and `lr` where they are not NULL (the caller changes them between replays).
- * Tensors of the list must not overlap.  Pointers need their element's alignment; 16 bytes make the accesses wide.
+ * Tensors of the list must not overlap.  Pointers need their element's alignment; 32 bytes (float) and 16 (bfloat16) make the accesses wide.
  * sb_adamw_moments writes what 8-bit moments stand for as bfloat16 (exact) to m_out[i] and v_out[i] (HOST arrays of DEVICE pointers).
  */
 typedef struct {

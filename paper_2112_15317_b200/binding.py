@@ -407,7 +407,7 @@ class AdamW:
                     setattr(e, name + "_scale", _dense(f"{name}_scale[{i}]", scale[i], (-(-k // 256),), torch.float32, dev))
             if shadows is not None:
                 e.shadow = _dense(f"shadows[{i}]", shadows[i], p.shape, torch.bfloat16, dev)
-        self.device = dev
+        self.device, self._room = dev, None
         self.set_grads(grads)
 
     def set_grads(self, grads):
@@ -432,8 +432,14 @@ class AdamW:
         """What the 8-bit moments stand for: two lists of bf16 tensors."""
         torch, params = self._t[:2]
         _, here, stream = _on_device(params[0])
+        if self._room is None:        # every tensor's place in one buffer, 16 bytes apart at least, and the pieces it is cut into
+            sizes = [p.numel() for p in params]
+            self._room = [n for k in sizes for n in (k, -k % 8)]
         with here:
-            out = [[torch.empty(p.shape, dtype=torch.bfloat16, device=self.device) for p in params] for _ in range(2)]
+            out = []
+            for side in range(2):
+                flat = torch.empty(sum(self._room), dtype=torch.bfloat16, device=self.device)
+                out.append([t if p.dim() == 1 else t.view(p.shape) for t, p in zip(flat.split(self._room)[::2], params)])
             ptrs = [(c_void_p * len(params))(*[t.data_ptr() for t in side]) for side in out]
             _check(sb_adamw_moments(self._list, len(self._list), byref(self.cfg), *ptrs, stream))
         return out
