@@ -59,7 +59,7 @@ typedef enum {
     SB_FC_RELU_WHOLE = 6, /* SB_FC_RELU kept whole on every worker: the "do not partition" outcome of the paper's
                              computation-to-communication test for this layer [Layer Partitioning] */
     SB_FC_WHOLE = 7,      /* SB_FC (logits layer) kept whole */
-    SB_DROPOUT = 8        /* dropout on the output of the SB_FC_RELU / SB_FC_RELU_WHOLE layer directly below it: a one-to-one
+    SB_DROPOUT = 8,       /* dropout on the output of the SB_FC_RELU / SB_FC_RELU_WHOLE layer directly below it: a one-to-one
                              functional layer that follows the partitioned width, no modulo or shard node in between [Listing 1,
                              case DROPOUT | RELU].  `out` = drop probability p in units of 1/65536 (1..65535).  Element (batch row
                              g, column c) of the layer's [B, width] input is kept iff the first output word of the
@@ -70,6 +70,13 @@ typedef enum {
                              time a forward pass has run the network's last dropout layer (graph replays included); in
                              sb_modulo_step the K sub-iterations are one iteration and every example meets the mask of its
                              batch row. */
+    SB_GATED_FFN = 10     /* residual gated feed-forward block of hidden width `out` on the [B, D] features x of the layer below, kept whole on
+                             every worker: y = scale * x + gate * (w_post * N(Wd (silu(G) * U))), [G U] = Wgu (w_pre * N(x)), N(v) =
+                             v / sqrt(mean(v^2) + 1e-6) over a row (sb_norm_* and sb_ffn_* below; no counterpart in the paper).
+                             SB_T_WEIGHT: part 0 = Wgu [2*out, D], part 1 = Wd [D, out]; SB_T_BIAS: parts 0 .. 3 = w_pre, w_post, gate, scale,
+                             [D] each (gradients, moments and bf16 copies likewise).  Not the first layer, D at most 16384, not with
+                             SB_FLAG_MODULO_SCHEDULE.  SB_BF16: w_pre * N(x), the block's output before its norm, [G U], and the gradients of
+                             the first two and of x's residual are stored in bfloat16; the vectors are float. */
 } sb_layer_kind;
 
 typedef struct {
@@ -93,9 +100,11 @@ enum {
     SB_FLAG_NO_HALO = 32,    /* 3x3 forward / data-gradient GEMMs on the kernel that fetches an activation box per filter tap
                                 instead of the default one that shares a fetch of bh + 2 image rows between the three taps of
                                 a filter column (for tests: both kernels must give the same results) */
-    SB_FLAG_FORCE_PERSIST = 64 /* 3x3 forward / data-gradient GEMMs on the persistent kernels (a few CTAs walk all output tiles, accumulators
+    SB_FLAG_FORCE_PERSIST = 64, /* 3x3 forward / data-gradient GEMMs on the persistent kernels (a few CTAs walk all output tiles, accumulators
                                 in turn) and weight gradients of up to 64 channels with all taps in one CTA, whatever the layer's
                                 size; by default only layers of many tiles use them (for tests at small sizes) */
+    SB_FLAG_ADAMW = 128     /* updates are sb_adamw_step's: reserves the second moments (SB_T_VAR_*; SB_T_MOM_* are then the first moments); the calls that
+                                update by SGD return SB_ERR_STATE */
 };
 
 typedef struct {
@@ -123,7 +132,9 @@ enum {
     SB_T_POOL_IDX = 8, /* uint8 argmax position (dh*2+dw) per pooled element, replica `part` */
     SB_T_ROW_LOSS = 9, /* float [B]: per-row negative log-likelihood (layer = the loss layer) */
     SB_T_INPUT_GRAD = 10, /* gradient w.r.t. replica `part`'s input (needs SB_FLAG_INPUT_GRAD) */
-    SB_T_SHADOW_W = 11 /* bf16 copy of the weight used by the contractions (SB_BF16 only) */
+    SB_T_SHADOW_W = 11, /* bf16 copy of the weight used by the contractions (SB_BF16 only) */
+    SB_T_VAR_W = 12,   /* second moments, float (SB_FLAG_ADAMW only) */
+    SB_T_VAR_B = 13
 };
 enum { SB_DT_F32 = 0, SB_DT_BF16 = 1, SB_DT_U8 = 2, SB_DT_I32 = 3 };
 
@@ -131,7 +142,7 @@ enum { SB_DT_F32 = 0, SB_DT_BF16 = 1, SB_DT_U8 = 2, SB_DT_I32 = 3 };
  * Size of the device arena a model needs.  [Design: the model builder supplies a sequential
  * layer list, the batch size and the MP group size.]
  *   layers, cfg : host pointers.  arena_bytes : host pointer, receives the size.
- * Validation (SB_ERR_SHAPE): conv/pool layers first, then FC layers, then exactly one loss
+ * Validation (SB_ERR_SHAPE): conv/pool layers first, then FC layers (and what goes between them), then exactly one loss
  * whose class count equals the last FC width; H and W even at every pool; 1 <= R,K <= 64;
  * K <= every FC width.
  */
@@ -544,6 +555,9 @@ typedef struct {
     const float* dev_lr;
 } sb_adamw_hyper;
 sb_status sb_adamw_tensors(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, const sb_adamw_hyper* hyper, int64_t step, void* stream);
+/* AdamW on every parameter of a model created with SB_FLAG_ADAMW (SB_ERR_STATE otherwise), from the gradients of the last sb_backward, in place of
+ * sb_sgd_step; in SB_BF16 mode also refreshes the bf16 weight copies.  Float moments; hyper and step as above. */
+sb_status sb_adamw_step(sb_model* m, const sb_adamw_hyper* hyper, int64_t step, void* stream);
 sb_status sb_adamw_moments(const sb_adamw_tensor* list, int32_t n, const sb_adamw_config* cfg, void* const* m_out, void* const* v_out, void* stream);
 
 #ifdef __cplusplus

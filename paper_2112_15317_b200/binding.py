@@ -21,12 +21,12 @@ LIB_PATH = os.path.join(HERE, "libsplitbrain.so")
 
 SB_OK = 0
 SB_FP32, SB_BF16 = 0, 1
-SB_CONV3X3_RELU, SB_MAXPOOL2, SB_FC_RELU, SB_FC, SB_SOFTMAX_XENT, SB_FC_RELU_WHOLE, SB_FC_WHOLE, SB_DROPOUT = 1, 2, 3, 4, 5, 6, 7, 8
+SB_CONV3X3_RELU, SB_MAXPOOL2, SB_FC_RELU, SB_FC, SB_SOFTMAX_XENT, SB_FC_RELU_WHOLE, SB_FC_WHOLE, SB_DROPOUT, SB_GATED_FFN = 1, 2, 3, 4, 5, 6, 7, 8, 10
 SB_NODE_LAYER, SB_NODE_MODULO, SB_NODE_SHARD = 0, 1, 2
 SB_X_GATHER_ROWS, SB_X_GATHER_COLS, SB_X_REDUCE_COLS, SB_X_REDUCE_ROWS, SB_X_ALLREDUCE, SB_X_ALLREDUCE_GROUPS = 1, 2, 3, 4, 5, 6
-SB_FLAG_INPUT_GRAD, SB_FLAG_FORCE_SIMT, SB_FLAG_PROFILE_LAYERS, SB_FLAG_FORCE_PAIR, SB_FLAG_MODULO_SCHEDULE, SB_FLAG_NO_HALO, SB_FLAG_FORCE_PERSIST = 1, 2, 4, 8, 16, 32, 64
+SB_FLAG_INPUT_GRAD, SB_FLAG_FORCE_SIMT, SB_FLAG_PROFILE_LAYERS, SB_FLAG_FORCE_PAIR, SB_FLAG_MODULO_SCHEDULE, SB_FLAG_NO_HALO, SB_FLAG_FORCE_PERSIST, SB_FLAG_ADAMW = 1, 2, 4, 8, 16, 32, 64, 128
 (SB_T_WEIGHT, SB_T_BIAS, SB_T_GRAD_W, SB_T_GRAD_B, SB_T_MOM_W, SB_T_MOM_B, SB_T_ACT, SB_T_DACT,
- SB_T_POOL_IDX, SB_T_ROW_LOSS, SB_T_INPUT_GRAD, SB_T_SHADOW_W) = range(12)
+ SB_T_POOL_IDX, SB_T_ROW_LOSS, SB_T_INPUT_GRAD, SB_T_SHADOW_W, SB_T_VAR_W, SB_T_VAR_B) = range(14)
 SB_DT_F32, SB_DT_BF16, SB_DT_U8, SB_DT_I32 = 0, 1, 2, 3
 SB_ACT_SILU, SB_ACT_GELU, SB_ACT_RELU = 0, 1, 2
 SB_NORM_RMS, SB_NORM_LAYER = 0, 1
@@ -129,6 +129,7 @@ def _load():
         "sb_norm_forward": [P(sb_norm_config)] + [c_void_p] * 10,
         "sb_norm_backward": [P(sb_norm_config)] + [c_void_p] * 16 + [c_size_t, c_void_p],
         "sb_adamw_tensors": [P(sb_adamw_tensor), c_int32, P(sb_adamw_config), P(sb_adamw_hyper), c_int64, c_void_p],
+        "sb_adamw_step": [c_void_p, P(sb_adamw_hyper), c_int64, c_void_p],
         "sb_adamw_moments": [P(sb_adamw_tensor), c_int32, P(sb_adamw_config), P(c_void_p), P(c_void_p), c_void_p],
         "sb_profile_begin": [c_void_p, c_void_p],
         "sb_profile_end": [c_void_p, c_void_p, P(sb_profile_entry), c_int32, P(c_int32)],
@@ -187,6 +188,7 @@ sb_norm_forward = _lib.sb_norm_forward
 sb_norm_backward = _lib.sb_norm_backward
 sb_adamw_tensors = _lib.sb_adamw_tensors
 sb_adamw_moments = _lib.sb_adamw_moments
+sb_adamw_step = _lib.sb_adamw_step
 sb_partition = _lib.sb_partition
 sb_exchange_plan = _lib.sb_exchange_plan
 
@@ -478,6 +480,10 @@ def bf16_bits_to_f32(a: np.ndarray) -> np.ndarray:
     return (a.astype(np.uint32) << 16).view(np.float32)
 
 
+# parts of a SB_GATED_FFN layer's SB_T_WEIGHT and SB_T_BIAS tensors, and their names in load_params / gather_params
+GATED_WEIGHTS, GATED_VECTORS = ("gate_up", "down"), ("w_pre", "w_post", "gate", "scale")
+
+
 class Model:
     """Owns the device arena (a torch uint8 tensor) and the sb_model handle."""
 
@@ -555,6 +561,11 @@ class Model:
 
     def sgd_step(self, lr, momentum):
         _check(sb_sgd_step(self.h, c_float(lr), c_float(momentum), self._stream()))
+
+    def adamw_step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
+        """AdamW from the gradients of backward() (model created with SB_FLAG_ADAMW); dev_step / dev_lr as for AdamW.step."""
+        h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _address(dev_step), _address(dev_lr))
+        _check(sb_adamw_step(self.h, byref(h), c_int64(step), self._stream()))
 
     def loss(self) -> float:
         v = c_float()
@@ -644,6 +655,11 @@ class Model:
                 for j in range(K):
                     self.write(SB_T_WEIGHT, li, j, p["w"][cb[j]:cb[j + 1]])
                     self.write(SB_T_BIAS, li, j, p["b"][cb[j]:cb[j + 1]])
+            elif kind == SB_GATED_FFN:
+                for j, name in enumerate(GATED_WEIGHTS):
+                    self.write(SB_T_WEIGHT, li, j, p[name])
+                for j, name in enumerate(GATED_VECTORS):
+                    self.write(SB_T_BIAS, li, j, p[name])
         self.refresh_shadow()
         self.torch.cuda.synchronize()
 
@@ -658,6 +674,9 @@ class Model:
                 ws = [self.read(what_w, li, j, squeeze=False)[:, :, 0, 0] for j in range(K)]
                 bs = [self.read(what_b, li, j, squeeze=False)[:, 0, 0, 0] for j in range(K)]
                 out.append({"w": np.concatenate(ws, 0), "b": np.concatenate(bs, 0)})
+            elif kind == SB_GATED_FFN:
+                out.append({**{n: self.read(what_w, li, j, squeeze=False)[:, :, 0, 0] for j, n in enumerate(GATED_WEIGHTS)},
+                            **{n: self.read(what_b, li, j, squeeze=False)[:, 0, 0, 0] for j, n in enumerate(GATED_VECTORS)}})
             else:
                 out.append(None)
         return out

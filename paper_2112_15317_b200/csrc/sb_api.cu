@@ -12,6 +12,8 @@
 #include "../../include/splitbrain.h"
 #include "sb_internal.h"
 #include "sb_umma.h"
+#include "sb_ffn.h"
+#include "sb_norm.h"
 
 #include <cstdarg>
 #include <cstdio>
@@ -60,6 +62,11 @@ struct Layer {
     char* act = nullptr;                        // [B, out_per_img] activation dtype (float for the logits layer)
     char* dact = nullptr;                       // same shape, activation dtype
     uint8_t* idx = nullptr;                     // pool argmax
+    // gated feed-forward block (in_f = out_f = its width, out = the hidden width): the down-projection's weights begin p_w2 in the parameter
+    // regions, its four vectors `vec` apart from p_b; what its forward pass keeps, and gradients on the way
+    size_t p_w2 = 0, vec = 0;
+    char *blk_n = nullptr, *blk_f = nullptr, *blk_gu = nullptr;      // w_pre * N(x), the block's output before its norm, GU
+    float* blk_stats = nullptr;                                      // [2][B][4]
     bool thin_input = false;                    // conv with Cin of 1/3/4: dedicated input-layer kernels
     bool narrow = false;                        // FC with out <= 16: dedicated narrow kernels
     int K = 1;                                  // FC: column shards of this layer (the model's K, or 1 for a layer kept whole)
@@ -86,6 +93,10 @@ struct sb_model {
     size_t arena_bytes = 0;
     size_t P = 0;  // padded parameter element count
     float *Wm = nullptr, *Vm = nullptr, *Gm = nullptr;
+    float* Am = nullptr;              // second moments (SB_FLAG_ADAMW; Vm then holds the first)
+    char* blk_ws = nullptr;           // workspace of the gated blocks' calls, one after the other on the chain stream; gradients of blk_n and blk_f
+    size_t blk_ws_bytes = 0;
+    char *blk_dn = nullptr, *blk_df = nullptr;
     __nv_bfloat16* Sm = nullptr;
     __nv_bfloat16* Tm = nullptr;      // float mode: the conv weights as three planes of bf16 terms (launch_split_weights), t_n elements a plane
     size_t t_n = 0;                   // (the conv layers' parameters lie first in the parameter regions)
@@ -271,6 +282,10 @@ size_t contract_plan_layer(sb_model* m, int i, size_t max_part_floats)
     return need;
 }
 
+// Configurations of a gated block's calls
+sb_ffn_config block_ffn(const sb_model* m, const Layer& l) { return sb_ffn_config{m->B, l.in_f, l.out, SB_ACT_SILU, m->cfg.precision, SB_DT_F32}; }
+sb_norm_config block_norm(const sb_model* m, const Layer& l) { return sb_norm_config{m->B, 1, l.in_f, SB_NORM_RMS, m->cfg.precision, 1e-6f}; }
+
 // Walks the layer list, fills shapes, and assigns arena offsets (relative to base, which may be
 // null for a pure size computation).  Returns SB_OK and the total size.
 sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m, char* base, size_t* total)
@@ -335,6 +350,18 @@ sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m,
             l.out_per_img = (size_t)feat;
             m->last_dropout = i;
             break;
+        case SB_GATED_FFN:
+            if (i == 0 || m->L[i - 1].kind == SB_FC) return fail(SB_ERR_UNSUPPORTED, "layer %d: a gated feed-forward block goes between the first layer and the logits", i);
+            if (l.out < 1) return fail(SB_ERR_SHAPE, "layer %d: the hidden width must be positive", i);
+            if (feat < 0) { feat = (long)H * W * C; first_fc = i; }
+            if (feat > 16384) return fail(SB_ERR_UNSUPPORTED, "layer %d: a gated feed-forward block of width %ld (at most 16384)", i, feat);
+            if (cfg->flags & SB_FLAG_MODULO_SCHEDULE) return fail(SB_ERR_UNSUPPORTED, "layer %d: the modulo schedule has no gated feed-forward blocks", i);
+            l.in_f = l.out_f = (int)feat;
+            l.out_per_img = (size_t)feat;
+            l.vec = align_up((size_t)feat, 64);
+            l.n_w = align_up((size_t)2 * l.out * feat, 64) + (size_t)l.out * feat;
+            l.n_b = 4 * l.vec;
+            break;
         case SB_SOFTMAX_XENT:
             if (i != n - 1) return fail(SB_ERR_SHAPE, "the loss must be the last layer");
             if (i == 0 || m->L[i - 1].kind != SB_FC) return fail(SB_ERR_SHAPE, "the loss must follow an SB_FC (logits) layer");
@@ -348,6 +375,7 @@ sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m,
         if (l.n_w) {
             l.p_w = P; P += align_up(l.n_w, 64);
             l.p_b = P; P += align_up(l.n_b, 64);
+            if (l.kind == SB_GATED_FFN) l.p_w2 = l.p_w + align_up((size_t)2 * l.out * l.in_f, 64);
         }
     }
     if (m->L[n - 1].kind != SB_SOFTMAX_XENT) return fail(SB_ERR_SHAPE, "the last layer must be SB_SOFTMAX_XENT");
@@ -379,6 +407,7 @@ sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m,
     m->Wm = (float*)take(P * 4);
     m->Vm = (float*)take(P * 4);
     m->Gm = (float*)take(P * 4);
+    m->Am = (cfg->flags & SB_FLAG_ADAMW) ? (float*)take(P * 4) : nullptr;
     m->Sm = m->bf16 ? (__nv_bfloat16*)take(P * 2) : nullptr;
     scratch_region = true;      // from here on: activations, gradients of activations, scratch -- everything a step rewrites
     const size_t B = m->B;
@@ -390,6 +419,12 @@ sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m,
         l.act = take(B * l.out_per_img * e);
         l.dact = take(B * l.out_per_img * m->esz);
         if (l.kind == SB_MAXPOOL2) l.idx = (uint8_t*)take(B * l.out_per_img);
+        if (l.kind == SB_GATED_FFN) {
+            l.blk_n = take(B * l.in_f * m->esz);
+            l.blk_f = take(B * l.in_f * m->esz);
+            l.blk_gu = take(B * 2 * l.out * m->esz);
+            l.blk_stats = (float*)take(2 * B * 4 * sizeof(float));
+        }
         if (l.kind == SB_FC_RELU || l.kind == SB_FC) l.narrow = fc_narrow_supported(l.out_f, (int)B);
         if (l.kind == SB_CONV3X3_RELU) {
             l.thin_input = conv_in_supported(l.Cin, l.Cout);
@@ -414,6 +449,24 @@ sb_status plan(const sb_layer* layers, int n, const sb_config* cfg, sb_model* m,
     m->ws = (float*)take(ws_floats * 4);
     for (int k = 0; k < sb_model::MAX_WSTREAMS; ++k) m->ws_wk[k] = (float*)take(ws_floats * 4);
     m->ws_w = m->ws_wk[0];
+    {
+        size_t ws = 0, grad = 0;
+        for (int i = 0; i < n; ++i) {
+            const Layer& l = m->L[i];
+            if (l.kind != SB_GATED_FFN) continue;
+            const sb_ffn_config fc = block_ffn(m, l);
+            const sb_norm_config nc = block_norm(m, l);
+            for (int pass = 0; pass < 3; ++pass) {
+                size_t need = 0;
+                const sb_status s = pass < 2 ? sb_ffn_bytes(&fc, pass, &need) : sb_norm_bytes(&nc, &need);
+                if (s != SB_OK) return s;
+                ws = std::max(ws, need);
+            }
+            grad = std::max(grad, B * l.in_f * m->esz);
+        }
+        m->blk_ws_bytes = ws;
+        if (ws) { m->blk_ws = take(ws); m->blk_dn = take(grad); m->blk_df = take(grad); }
+    }
     m->row_loss = (float*)take(B * 4);
     scratch_region = false;     // (loss, counter and status words keep their values between calls)
     m->loss = (float*)take(256);              // [0] = mean loss, [1] = device status word: adjacent, so that one copy reads both back
@@ -466,6 +519,24 @@ inline int shard_lo(int j, int total, int K) { return (int)(((long)j * total) / 
                             if (rec_.e0) cudaEventRecord(rec_.e0, st); }                          \
         sb_status s_ = (expr);                                                                    \
         if (s_ != SB_OK) return fail(s_, "%s", umma_last_error());                                                            \
+        if (m->profiling && rec_.e1) { cudaEventRecord(rec_.e1, st); m->recs.push_back(rec_); }   \
+        if (m->debug_sync) {                                                                      \
+            cudaError_t d_ = cudaStreamSynchronize(st);                                           \
+            if (d_ != cudaSuccess) return fail(SB_ERR_CUDA, "kernel %s failed: %s", tag, cudaGetErrorString(d_)); \
+        }                                                                                         \
+    } while (0)
+
+// And for the operators' calls (n launches each), whose kernels report to the model's status word.
+#define O_TRY(tag, flops, bytes, n, expr)                                                         \
+    do {                                                                                          \
+        sb_model::Rec rec_{tag, nullptr, nullptr, (double)(flops), (double)(bytes), m->cur_layer}; \
+        if (m->profiling) { rec_.e0 = m->next_event(); rec_.e1 = m->next_event();                 \
+                            if (rec_.e0) cudaEventRecord(rec_.e0, st); }                          \
+        ops_status_of_model() = m->status;                                                        \
+        const sb_status s_ = (expr);                                                              \
+        ops_status_of_model() = nullptr;                                                          \
+        if (s_ != SB_OK) return s_;                                                               \
+        m->launches += n;                                                                         \
         if (m->profiling && rec_.e1) { cudaEventRecord(rec_.e1, st); m->recs.push_back(rec_); }   \
         if (m->debug_sync) {                                                                      \
             cudaError_t d_ = cudaStreamSynchronize(st);                                           \
@@ -649,6 +720,21 @@ sb_status forward_layer(sb_model* m, int i, cudaStream_t st)
             L_TRY("dropout_state", 0.0, 8.0, launch_dropout_state(m->drop_state, 1, 0, 0, st));
         break;
     }
+    case SB_GATED_FFN: {
+        const void* x = layer_input(m, i);
+        const float* v = m->Wm + l.p_b;
+        const sb_ffn_config fc = block_ffn(m, l);
+        sb_norm_config pre = block_norm(m, l), post = pre;
+        pre.groups = 0;
+        const void *wgu = wts, *wd = bf ? (const void*)(m->Sm + l.p_w2) : (const void*)(m->Wm + l.p_w2);
+        const double act = (double)B * l.in_f * e, hid = (double)B * l.out * e;
+        float* st2 = l.blk_stats + (size_t)B * 4;
+        O_TRY("block_norm", 0.0, 2.0 * act, 1, sb_norm_forward(&pre, x, v, nullptr, nullptr, nullptr, nullptr, nullptr, l.blk_n, l.blk_stats, st));
+        O_TRY("block_ffn_fwd", 6.0 * B * l.in_f * (double)l.out, 2.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * e, 2,
+              sb_ffn_forward(&fc, l.blk_n, wgu, wd, l.blk_gu, l.blk_f, m->blk_ws, m->blk_ws_bytes, st));
+        O_TRY("block_norm", 0.0, 3.0 * act, 1, sb_norm_forward(&post, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, l.act, nullptr, st2, st));
+        break;
+    }
     case SB_SOFTMAX_XENT: {
         if (!m->have_labels) return fail(SB_ERR_STATE, "the loss layer needs label pointers");
         const XentArgs a = xent_args(m, i);
@@ -777,6 +863,27 @@ sb_status backward_layer(sb_model* m, int i, cudaStream_t st, int part = SIDE_BO
         }
         break;
     }
+    case SB_GATED_FFN: {
+        // everything on the chain: the weight gradients come from the kernel that also computes the block's input gradient
+        if (!(part & SIDE_D)) break;
+        const void* x = layer_input(m, i);
+        const float* v = m->Wm + l.p_b;
+        float* dv = m->Gm + l.p_b;
+        const sb_ffn_config fc = block_ffn(m, l);
+        sb_norm_config pre = block_norm(m, l), post = pre;
+        pre.groups = 0;
+        const void *wgu = wts, *wd = bf ? (const void*)(m->Sm + l.p_w2) : (const void*)(m->Wm + l.p_w2);
+        const double act = (double)B * l.in_f * e, hid = (double)B * l.out * e;
+        const float* st2 = l.blk_stats + (size_t)B * 4;
+        O_TRY("block_norm_bwd", 0.0, 5.0 * act, 2, sb_norm_backward(&post, l.dact, nullptr, st2, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, d_below, m->blk_df,
+                                                                     nullptr, dv + l.vec, dv + 2 * l.vec, dv + 3 * l.vec, m->blk_ws, m->blk_ws_bytes, st));
+        O_TRY("block_ffn_bwd", 12.0 * B * l.in_f * (double)l.out, 3.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * (e + 4.0), 2,
+              sb_ffn_backward(&fc, m->blk_df, l.blk_n, l.blk_gu, wgu, wd, m->blk_dn, m->Gm + l.p_w, m->Gm + l.p_w2, m->blk_ws, m->blk_ws_bytes, st));
+        // the residual's gradient, so far in d_below, goes through the first norm in place
+        O_TRY("block_norm_bwd", 0.0, 4.0 * act, 2, norm_backward(&pre, d_below, m->blk_dn, l.blk_stats, x, v, nullptr, nullptr, nullptr, nullptr, d_below, nullptr,
+                                                                  dv, nullptr, nullptr, nullptr, m->blk_ws, m->blk_ws_bytes, below_relu, st));
+        break;
+    }
     case SB_DROPOUT: {
         // the layer above wrote the gradient w.r.t. this layer's output, zeroed wherever the output is zero (dropped, or the
         // ReLU below was inactive): what is left is the scale of the kept elements, and the result is the gradient w.r.t. the
@@ -890,9 +997,17 @@ sb_status resolve(sb_model* m, int what, int li, int part, char** ptr, int64_t s
     char* p = nullptr;
     int dt = SB_DT_F32;
     const bool is_conv = l.kind == SB_CONV3X3_RELU, is_fc = l.kind == SB_FC_RELU || l.kind == SB_FC, is_pool = l.kind == SB_MAXPOOL2;
-    const bool is_flat = is_fc || l.kind == SB_DROPOUT;   // [B, width] activations
+    const bool is_block = l.kind == SB_GATED_FFN;
+    const bool is_flat = is_fc || is_block || l.kind == SB_DROPOUT;   // [B, width] activations
     auto param = [&](float* region, bool weight) -> sb_status {
-        if (!is_conv && !is_fc) return fail(SB_ERR_INVALID_ARG, "layer %d has no parameters", li);
+        if (!is_conv && !is_fc && !is_block) return fail(SB_ERR_INVALID_ARG, "layer %d has no parameters", li);
+        if (is_block) {
+            if (part < 0 || part >= (weight ? 2 : 4)) return fail(SB_ERR_INVALID_ARG, "part %d out of range", part);
+            if (!weight) { p = (char*)(region + l.p_b + part * l.vec); sh[0] = l.in_f; }
+            else if (part == 0) { p = (char*)(region + l.p_w); sh[0] = 2 * l.out; sh[1] = l.in_f; }
+            else { p = (char*)(region + l.p_w2); sh[0] = l.in_f; sh[1] = l.out; }
+            return SB_OK;
+        }
         if (is_conv) {
             if (part != 0) return fail(SB_ERR_INVALID_ARG, "conv parameters are replicated: part must be 0");
             if (weight) { p = (char*)(region + l.p_w); sh[0] = l.Cout; sh[1] = 3; sh[2] = 3; sh[3] = l.Cin; }
@@ -913,6 +1028,11 @@ sb_status resolve(sb_model* m, int what, int li, int part, char** ptr, int64_t s
     case SB_T_GRAD_B: s = param(m->Gm, false); break;
     case SB_T_MOM_W: s = param(m->Vm, true); break;
     case SB_T_MOM_B: s = param(m->Vm, false); break;
+    case SB_T_VAR_W:
+    case SB_T_VAR_B:
+        if (!m->Am) return fail(SB_ERR_INVALID_ARG, "model was created without SB_FLAG_ADAMW");
+        s = param(m->Am, what == SB_T_VAR_W);
+        break;
     case SB_T_SHADOW_W:
         if (!m->bf16) return fail(SB_ERR_INVALID_ARG, "no bf16 weight copies in SB_FP32 mode");
         s = param(m->Wm, true);
@@ -1414,6 +1534,15 @@ static sb_status backward_pass(sb_model* m, cudaStream_t st, bool fuse_update, H
         } else {
             sb_status s = chain_bwd(m, i, st, SIDE_BOTH);
             if (s != SB_OK) return s;
+            if (two_streams && l.kind == SB_GATED_FFN) {
+                if (fuse) {
+                    CU_TRY(cudaEventRecord(m->ev_dgrad[i], st));
+                    s = update_aside(i, st);
+                    if (s != SB_OK) return s;
+                }
+                s = held_weight_side();
+                if (s != SB_OK) return s;
+            }
         }
     }
     {
@@ -1551,9 +1680,25 @@ static sb_status modulo_step_direct(sb_model* m, const void* const* x, const int
     return SB_OK;
 }
 
+static sb_status refuse_sgd() { return fail(SB_ERR_STATE, "the model was created with SB_FLAG_ADAMW: its updates are sb_adamw_step's"); }
+
+sb_status sb_adamw_step(sb_model* m, const sb_adamw_hyper* hyper, int64_t step, void* stream)
+{
+    if (!m) return fail(SB_ERR_INVALID_ARG, "null model");
+    if (!m->Am) return fail(SB_ERR_STATE, "the model was created without SB_FLAG_ADAMW");
+    const sb_adamw_tensor t{m->Wm, m->Gm, m->Vm, m->Am, nullptr, nullptr, m->Sm, (int64_t)m->P};
+    const sb_adamw_config c{0, 32, SB_DT_F32};
+    cudaStream_t st = (cudaStream_t)stream;
+    m->cur_layer = -1;
+    O_TRY("adamw", 0.0, (double)m->P * (m->bf16 ? 30.0 : 28.0), 1, sb_adamw_tensors(&t, 1, &c, hyper, step, stream));
+    m->last_step_launches = m->launches;
+    return SB_OK;
+}
+
 sb_status sb_sgd_step(sb_model* m, float lr, float momentum, void* stream)
 {
     if (!m) return fail(SB_ERR_INVALID_ARG, "null model");
+    if (m->Am) return refuse_sgd();
     return update_all(m, Hyper{lr, momentum, nullptr}, (cudaStream_t)stream);
 }
 
@@ -1649,6 +1794,7 @@ static sb_status graph_replay(sb_model* m, sb_model::StepGraph& G, StepFn step, 
 sb_status sb_graph_step(sb_model* m, const void* const* x, const int32_t* const* labels, float lr, float momentum, void* stream)
 {
     if (!m) return fail(SB_ERR_INVALID_ARG, "null model");
+    if (m->Am) return refuse_sgd();
     sb_status s = graph_replay(m, m->g_dev, whole_step, x, labels, lr, momentum, stream);
     if (s == SB_OK) m->have_fwd = true;
     return s;
@@ -1658,6 +1804,7 @@ sb_status sb_modulo_step(sb_model* m, const void* const* x, const int32_t* const
 {
     if (!m) return fail(SB_ERR_INVALID_ARG, "null model");
     if (!(m->cfg.flags & SB_FLAG_MODULO_SCHEDULE)) return fail(SB_ERR_STATE, "the model was created without SB_FLAG_MODULO_SCHEDULE");
+    if (m->Am) return refuse_sgd();
     m->g_mod.priorities = true;
     sb_status s = graph_replay(m, m->g_mod, modulo_step_direct, x, labels, lr, momentum, stream);
     if (s == SB_OK) m->have_fwd = false;
@@ -1718,6 +1865,7 @@ static sb_status host_step(sb_model* m, const void* host_x, const int32_t* host_
                            float* host_loss)
 {
     cudaStream_t st = (cudaStream_t)stream;
+    if (m->Am) return refuse_sgd();
     sb_status hs = host_step_objects(m);
     if (hs != SB_OK) return hs;
     const size_t xb = (size_t)m->B * m->in_per_img * m->esz;
@@ -1879,6 +2027,7 @@ sb_status sb_param_bytes(const sb_model* m, int32_t shard, size_t* bytes)
             size_t rows = l.K == 1 ? (size_t)l.out_f : (size_t)(shard_lo(shard + 1, l.out_f, l.K) - shard_lo(shard, l.out_f, l.K));
             n += rows * l.in_f + rows;
         }
+        else if (l.kind == SB_GATED_FFN) n += 3 * (size_t)l.out * l.in_f + 4 * (size_t)l.in_f;
     }
     *bytes = n * 4;
     return SB_OK;

@@ -199,6 +199,7 @@ static __device__ uint32_t g_ops_status;
 // (the address is looked up once per device)
 uint32_t* ops_status()
 {
+    if (ops_status_of_model()) return ops_status_of_model();
     static uint32_t* at[64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;

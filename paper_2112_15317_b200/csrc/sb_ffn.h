@@ -7,7 +7,9 @@
 namespace sb {
 
 // Device status word of the operators that have no model: an array of the library's image, so that a call needs no memory of its own for it.
+// (a model's own word, while the calling thread has set one)
 uint32_t* ops_status();
+inline uint32_t*& ops_status_of_model() { static thread_local uint32_t* word = nullptr; return word; }
 
 #ifdef __CUDACC__
 // a(g).  EXACT: library exp and division; otherwise their approximations (errors of 2^-21, for results that bf16 rounds).

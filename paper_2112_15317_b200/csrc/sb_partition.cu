@@ -94,6 +94,14 @@ sb_status walk(const sb_layer* layers, int32_t n, const sb_config* cfg, std::vec
                 return fail(SB_ERR_UNSUPPORTED, "layer %d: dropout must follow an FC + ReLU layer", i);
             if (out < 1 || out > 65535) return fail(SB_ERR_SHAPE, "layer %d: drop probability must be 1..65535 (units of 1/65536)", i);
             push(SB_NODE_LAYER, i, dim != dimF ? K : 1, dim, dimF);
+        } else if (kind == SB_GATED_FFN) {
+            // kept whole: needs the full width, and passes it on
+            if (i == 0) return fail(SB_ERR_UNSUPPORTED, "layer 0 cannot be a gated feed-forward block");
+            if (out < 1) return fail(SB_ERR_SHAPE, "layer %d: the hidden width must be positive", i);
+            if (dim != dimF) push(SB_NODE_SHARD, i, K, dimF, dimF);
+            flat = true;
+            dim = dimF;
+            push(SB_NODE_LAYER, i, 1, dim, dimF);
         } else if (kind == SB_SOFTMAX_XENT) {
             if (dim != dimF) push(SB_NODE_SHARD, i, K, dimF, dimF);      // the loss needs the full width
             dim = dimF;
@@ -183,14 +191,15 @@ extern "C" sb_status sb_exchange_plan(const sb_layer* layers, int32_t n, const s
                     }
         } else {
             const int kind = layers[nd.layer].kind;
+            const bool fc = is_fc(kind) || kind == SB_GATED_FFN;
             // parameters that every worker holds AND trains on its own rows are reduced over all N workers: the conv stack, and
             // an FC layer kept whole below the modulo layer (every FC layer when K = 1).
-            const bool dp_params = kind == SB_CONV3X3_RELU || (is_fc(kind) && nd.shards == 1 && !gathered);
+            const bool dp_params = kind == SB_CONV3X3_RELU || (fc && nd.shards == 1 && !gathered);
             if (dp_params && N > 1) bwd_rev.push_back(msg(SB_X_ALLREDUCE, nd.layer, 1, -1, -1, 0, 0, 0, 0, 0));
             // above the modulo layer a group trains its FC parameters on the group's rows only: shard o is summed over the
             // workers at offset o of every group (src = o); a layer kept whole there is equal on all workers of a group and
             // is summed over the groups likewise (src = -1: every offset)
-            if (is_fc(kind) && !dp_params && G > 1) {
+            if (fc && !dp_params && G > 1) {
                 if (nd.shards > 1)
                     for (int o = 0; o < mp; ++o)
                         bwd_rev.push_back(msg(SB_X_ALLREDUCE_GROUPS, nd.layer, 1, o, -1, 0, 0, lo(o, nd.dimF, mp), lo(o + 1, nd.dimF, mp), nd.dimF));
