@@ -76,7 +76,8 @@ typedef enum {
                              SB_T_WEIGHT: part 0 = Wgu [2*out, D], part 1 = Wd [D, out]; SB_T_BIAS: parts 0 .. 3 = w_pre, w_post, gate, scale,
                              [D] each (gradients, moments and bf16 copies likewise).  Not the first layer, D at most 16384, not with
                              SB_FLAG_MODULO_SCHEDULE.  SB_BF16: w_pre * N(x), the block's output before its norm, [G U], and the gradients of
-                             the first two and of x's residual are stored in bfloat16; the vectors are float. */
+                             the first two and of x's residual are stored in bfloat16; the vectors are float.
+                             SB_FLAG_FORCE_SIMT does not change its kernels. */
 } sb_layer_kind;
 
 typedef struct {
@@ -503,7 +504,8 @@ sb_status sb_ffn_backward(const sb_ffn_config* cfg, const void* dy, const void* 
  * gate [groups, d]: row r uses gate row r / (rows / groups); groups = 0 without a gate.  w_post, scale, w_pre [d].
  *   stats [rows, 4] : float, 16-byte aligned, receives what the backward pass needs (mean and 1/deviation of f's and y's rows), or NULL.
  * Backward, from dy and dn (either may be NULL): dx and df (activation dtype), and the vectors' gradients (float, overwritten; sums over the
- * rows, dgate over each group's), any of which may be NULL.  y is computed again from x and f.  Same bits on every call.
+ * rows, dgate over each group's), any of which may be NULL.  y is computed again from x and f.  Same bits on every call.  dx may lie in dy's place;
+ * apart from that no output overlaps an input.
  *   ws : workspace of sb_norm_bytes bytes, 16-byte aligned.
  * SB_ERR_UNSUPPORTED: d above 16384.
  */

@@ -261,7 +261,8 @@ sb_status norm_backward(const sb_norm_config* c, const void* dy, const void* dn,
     p.status = ops_status();
     if (!p.status) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
     if (vec) { p.gate_ring = gate && p.per_group == 1; plan_ring(p, g, (int)e, pieces_of(c->d, vec) == 1 ? RING_LIMIT / 2 : RING_LIMIT); }
-    cudaError_t r = launch_norm_backward(p, c->precision == SB_BF16, c->kind == SB_NORM_LAYER, g.ctas, st);
+    cudaError_t r = c->precision == SB_BF16 ? launch_norm_backward_bf16(p, c->kind == SB_NORM_LAYER, g.ctas, st)
+                                             : launch_norm_backward_f32(p, c->kind == SB_NORM_LAYER, g.ctas, st);
     const bool gate_sum = dgate && t.per_group > 1;
     if (r == cudaSuccess && (want || gate_sum)) {
         const SumArgs a{part, gate_part, {dw_pre, dw_post, dscale}, dgate, g.ctas, t.per_group, c->groups, c->d};

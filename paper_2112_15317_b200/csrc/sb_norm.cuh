@@ -1,4 +1,4 @@
-// Device side of the norms around a block that both directions share (sb_norm.cu, sb_norm_backward.cu): parameters, how rows fall to CTAs, loads and stores
+// Device side of the norms around a block that both directions share (sb_norm.cu, sb_norm_backward.cuh): parameters, how rows fall to CTAs, loads and stores
 // of a thread's columns, sums over a team of warps, the ring of rows in shared memory.
 #pragma once
 
@@ -358,6 +358,7 @@ inline int by_of(const NormParams& p) { return !p.vec ? BY_ELEMENT : p.stages > 
 
 }  // namespace
 
-cudaError_t launch_norm_backward(const NormParams& p, bool bf16, bool layer, int64_t ctas, cudaStream_t st);
+cudaError_t launch_norm_backward_bf16(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st);
+cudaError_t launch_norm_backward_f32(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st);
 
 }  // namespace sb

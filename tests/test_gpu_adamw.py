@@ -305,6 +305,33 @@ def test_replayed_in_a_graph_with_its_step_in_device_memory(bits):
         assert np.array_equal(a, c)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_2_32_elements(bits):
+    """The end of a tensor of more than 2^32 elements: as in a tensor of its own (8 bits: with a gradient and moments whose codes need no rounding, since the
+    random bits go by the element's place)."""
+    import torch
+    b = sb()
+    n, tail = (1 << 32) + 700, 600 + 256          # (from a block's first element)
+    lo = n - tail - (n - tail) % 256
+    p, gr = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    p[lo:] = torch.randn(n - lo, generator=g, device="cuda")
+    gr[lo:] = torch.randn(n - lo, generator=g, device="cuda").sign().bfloat16()
+    state = [torch.zeros(n, dtype=torch.float32 if bits == 32 else torch.uint8, device="cuda") for _ in range(2)]
+    scale = [torch.ones(-(-n // 256), device="cuda") for _ in range(2)] if bits == 8 else [None, None]
+    cut = lambda t, k=lo: None if t is None else t[k:].clone()  # noqa: E731
+    small = [cut(p), cut(gr), *[cut(t) for t in state], *[cut(t, lo // 256) for t in scale]]
+    wrap = lambda t: None if t is None else [t]  # noqa: E731
+    b.AdamW([p], [gr], *[[t] for t in state], *[wrap(t) for t in scale], seed=1).step(1e-2, beta1=0.5, beta2=0.5, step=1)
+    b.AdamW([small[0]], [small[1]], [small[2]], [small[3]], wrap(small[4]), wrap(small[5]), seed=1).step(1e-2, beta1=0.5, beta2=0.5, step=1)
+    assert torch.equal(p[lo:], small[0])
+    for t, u in zip(state, small[2:4]):
+        assert torch.equal(t[lo:], u)
+    for t, u in zip(scale, small[4:]):
+        assert t is None or torch.equal(t[lo // 256:], u)
+
+
 def test_refusals():
     import ctypes
     b = sb()

@@ -214,6 +214,26 @@ def test_streams_and_graphs(rows, bf16):
 
 
 @pytest.mark.gpu
+def test_more_than_2_32_elements():
+    """GU of more than 2^32 elements: the last rows as in a call of their own (the same kernel, whose rows do not depend on one another)."""
+    b = sb()
+    d, f, some = 64, 2048, 70000
+    rows = (1 << 32) // (2 * f) + some
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    x = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    x[-some:] = rnd(some, d)
+    wgu, wd = rnd(2 * f, d), rnd(d, f)
+    y, gu = b.ffn_forward(x, wgu, wd, save=True)
+    y2, gu2 = b.ffn_forward(x[-some:].clone(), wgu, wd, save=True)
+    assert torch.equal(y[-some:], y2) and torch.equal(gu[-some:], gu2)
+    dx = b.ffn_backward(x, x, gu, wgu, wd, needs=(True, False, False))[0]
+    dx2 = b.ffn_backward(x[-some:].clone(), x[-some:].clone(), gu2, wgu, wd, needs=(True, False, False))[0]
+    assert torch.equal(dx[-some:], dx2)
+    b.ops_check()
+
+
+@pytest.mark.gpu
 def test_no_rows():
     b = sb()
     x, wgu, wd, dy = inputs(0, 64, 128, True)

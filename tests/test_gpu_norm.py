@@ -237,6 +237,44 @@ def test_no_rows_and_other_streams():
         assert torch.equal(a, c)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 100, 4096])
+def test_addresses_that_are_not_aligned(d):
+    """Matrices and vectors one element behind an aligned address: the same values as at aligned ones, up to the order of the sums."""
+    b = sb()
+    for bf16 in (False, True):
+        t = gpu(inputs(40, d, bf16, 4, ALL))
+        off = {k: None if v is None else torch.cat([v.new_zeros(1), v.reshape(-1)])[1:].view(v.shape) for k, v in t.items()}
+        st, so = (b.norm_forward(*[c[k] for k in NAMES], save=True) for c in (t, off))
+        u = 2.0 ** -7 if bf16 else 2.0 ** -18          # a step of the result's type where a sum in another order falls to the other side; float: the sums' own bound
+        for p, q in zip(st[:2], so[:2]):
+            assert ((p.double() - q.double()).abs() <= u * (p.double().abs() + p.double().abs().mean())).all()
+        back, boff = b.norm_backward(t["dy"], t["dn"], st[2], *[t[k] for k in NAMES]), b.norm_backward(off["dy"], off["dn"], st[2], *[off[k] for k in NAMES])
+        for k, p in back.items():
+            tol = u if k in ("dx", "df") else 2.0 ** -18
+            assert ((p.double() - boff[k].double()).abs() <= tol * (p.double().abs() + 4 * p.double().abs().mean())).all(), k
+
+
+@pytest.mark.gpu
+def test_more_than_2_32_elements():
+    """Rows behind the 2^32nd element: the same bits as by themselves (a row's arithmetic does not depend on the number of rows)."""
+    b = sb()
+    rows, d, some = (1 << 32) // 1024 + 5000, 1024, 3000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(rows, d, dtype=torch.bfloat16, device="cuda")
+    x[:some].normal_(generator=g)
+    x[some:-some] = 0.5
+    x[-some:].normal_(generator=g)
+    w = torch.rand(d, generator=g, device="cuda")
+    _, n, st = b.norm_forward(x, w, save=True)
+    for part in (slice(0, some), slice(rows - some, rows)):
+        _, m, s2 = b.norm_forward(x[part].clone(), w, save=True)
+        assert torch.equal(n[part], m) and torch.equal(st[part], s2)
+    dx = b.norm_backward(None, x, st, x, w)["dx"]
+    m = b.norm_backward(None, x[-some:].clone(), st[-some:].clone(), x[-some:].clone(), w)["dx"]
+    assert torch.equal(dx[-some:], m)
+
+
 def test_refusals():
     b = sb()
     a, n = ctypes.c_void_p(0x1000), None
