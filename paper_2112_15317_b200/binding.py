@@ -388,12 +388,18 @@ class AdamW:
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, shadows=None, seed=0):
         import torch
+        params, grads, m, v, m_scale, v_scale, shadows = (None if x is None else list(x) for x in (params, grads, m, v, m_scale, v_scale, shadows))
         if not params:
             raise SBError(1, "an empty list of parameters")
-        self._t = (torch, params, m, v, m_scale, v_scale, shadows)
+        self._t = (torch, params, m, v, m_scale, v_scale, shadows)      # (lists of our own: the tensors live as long as their addresses are used)
         n, dev = len(params), params[0].device
         if not all(len(x) == n for x in (grads, m, v, m_scale, v_scale, shadows) if x is not None):
             raise SBError(1, "lists of different lengths")
+        if (m_scale is None) != (v_scale is None):
+            raise SBError(1, "scales for one of the two moments only")
+        held = [p.data_ptr() for p in params if p.numel()]
+        if len(set(held)) < len(held):
+            raise SBError(1, "a parameter is in the list twice")
         bits = 32 if m_scale is None else 8
         self._list = (sb_adamw_tensor * n)()
         self.cfg = sb_adamw_config(seed, bits, SB_DT_F32)
@@ -414,11 +420,15 @@ class AdamW:
 
     def set_grads(self, grads):
         torch, params = self._t[:2]
+        grads = list(grads)
+        if len(grads) != len(params):
+            raise SBError(1, f"{len(grads)} gradients for {len(params)} parameters")
         dtype = grads[0].dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise SBError(1, f"gradients: float32 or bfloat16, not {dtype}")
-        for i, (e, p, g) in enumerate(zip(self._list, params, grads)):
-            e.grad = _dense(f"grads[{i}]", g, p.shape, dtype, self.device)
+        ptrs = [_dense(f"grads[{i}]", g, p.shape, dtype, self.device) for i, (p, g) in enumerate(zip(params, grads))]
+        for e, ptr in zip(self._list, ptrs):         # (all or none)
+            e.grad = ptr
         self.cfg.grad_dtype = SB_DT_BF16 if dtype == torch.bfloat16 else SB_DT_F32
         self._grads = grads
 
@@ -564,7 +574,8 @@ class Model:
 
     def adamw_step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
         """AdamW from the gradients of backward() (model created with SB_FLAG_ADAMW); dev_step / dev_lr as for AdamW.step."""
-        h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _address(dev_step), _address(dev_lr))
+        torch, dev = self.torch, self.arena.device
+        h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _dense("dev_step", dev_step, (1,), torch.int64, dev), _dense("dev_lr", dev_lr, (1,), torch.float32, dev))
         _check(sb_adamw_step(self.h, byref(h), c_int64(step), self._stream()))
 
     def loss(self) -> float:

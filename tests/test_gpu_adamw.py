@@ -383,3 +383,39 @@ def test_binding_refusals():
         b.AdamW([p], [p], [p.to(torch.uint8)], [p.to(torch.uint8)], [torch.zeros(2)], [torch.zeros(1)])
     with pytest.raises(b.SBError):
         b.AdamW([p], [p], [p], [p]).step(1e-3)          # not on a CUDA device
+
+
+def test_binding_holds_what_it_has_addresses_of():
+    """The lists are the caller's to change: the tensors live on, and a call with unfit gradients leaves those of the call before."""
+    import gc
+    import weakref
+    import torch
+    b = sb()
+    lists = [[torch.zeros(8) for _ in range(2)] for _ in range(5)]          # p, g, m, v, shadows
+    lists[4] = [t.bfloat16() for t in lists[4]]
+    a = b.AdamW(*lists[:4], shadows=lists[4])
+    alive = [weakref.ref(t) for x in lists for t in x]
+    before = [e.grad for e in a._list]
+    for bad in ([torch.zeros(8)], [torch.zeros(8)] * 3, [torch.zeros(8), torch.zeros(4)], [torch.zeros(8), torch.zeros(8).bfloat16()], []):
+        with pytest.raises(b.SBError):
+            a.set_grads(bad)
+        assert [e.grad for e in a._list] == before and a.cfg.grad_dtype == b.SB_DT_F32
+    for x in lists:
+        x.clear()
+    gc.collect()
+    assert all(w() is not None for w in alive)
+    new = [torch.zeros(8).bfloat16() for _ in range(2)]
+    a.set_grads(iter(new))
+    assert [e.grad for e in a._list] == [t.data_ptr() for t in new] and a.cfg.grad_dtype == b.SB_DT_BF16
+
+
+def test_binding_refuses_a_parameter_twice_and_scales_of_one_moment():
+    import torch
+    b = sb()
+    p, q, c = torch.zeros(8), torch.zeros(8), torch.zeros(8, dtype=torch.uint8)
+    with pytest.raises(b.SBError):
+        b.AdamW([p, p], [q, q], [q, q], [q, q])
+    for scales in (([torch.zeros(1)], None), (None, [torch.zeros(1)])):
+        with pytest.raises(b.SBError):
+            b.AdamW([p], [q], [c], [c], *scales)
+    b.AdamW([torch.zeros(0), torch.zeros(0), p], [torch.zeros(0), torch.zeros(0), q], [torch.zeros(0), torch.zeros(0), q], [torch.zeros(0), torch.zeros(0), q])
