@@ -444,15 +444,27 @@ class AdamW:
         """What the 8-bit moments stand for: two lists of bf16 tensors."""
         torch, params = self._t[:2]
         _, here, stream = _on_device(params[0])
-        if self._room is None:        # every tensor's place in one buffer, 16 bytes apart at least, and the pieces it is cut into
-            sizes = [p.numel() for p in params]
-            self._room = [n for k in sizes for n in (k, -k % 8)]
+        if self._room is None:        # every tensor's place in one buffer, at a multiple of eight elements; the pieces it is cut into, those that are no gaps
+            pieces, places, starts, at = [], [], [], 0
+            for p in params:
+                k = p.numel()
+                places.append(len(pieces))
+                starts.append(2 * at)
+                pieces += [k, -k % 8] if k % 8 else [k]
+                at += k + -k % 8
+            flat = all(p.dim() == 1 for p in params)
+            self._room = at, pieces, places if len(places) < len(pieces) else None, starts, flat
+        total, pieces, places, starts, flat = self._room
+        out, ptrs = [], []
         with here:
-            out = []
             for side in range(2):
-                flat = torch.empty(sum(self._room), dtype=torch.bfloat16, device=self.device)
-                out.append([t if p.dim() == 1 else t.view(p.shape) for t, p in zip(flat.split(self._room)[::2], params)])
-            ptrs = [(c_void_p * len(params))(*[t.data_ptr() for t in side]) for side in out]
+                buf = torch.empty(total, dtype=torch.bfloat16, device=self.device)
+                views = buf.split(pieces)
+                if places is not None:
+                    views = [views[k] for k in places]
+                out.append(list(views) if flat else [t if p.dim() == 1 else t.view(p.shape) for t, p in zip(views, params)])
+                base = buf.data_ptr()
+                ptrs.append((c_void_p * len(params))(*[base + s for s in starts]))
             _check(sb_adamw_moments(self._list, len(self._list), byref(self.cfg), *ptrs, stream))
         return out
 

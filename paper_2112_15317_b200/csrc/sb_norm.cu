@@ -13,8 +13,8 @@
 // the two means in d, so that all sums of a row are taken in one round: with e = dy + inv_y dz,
 //   sum q d fhat = sum q e fhat - inv_y (mean(dz) sum q fhat + mean(dz yhat) sum q yhat fhat), and the same without fhat.
 //
-// What bounds it: HBM, each activation read or written once.  A row belongs to a team of warps, eight columns a thread (16 beyond 4096), so that a
-// CTA of 16 warps works on 1 to 16 rows at a time; a team takes consecutive rows, which come through a ring of bulk copies in shared memory, two
+// What bounds it: HBM, each activation read or written once.  A row belongs to a team of warps, 16 columns a thread (eight in rows of up to 256), so that
+// a CTA works on 1 to 16 rows at a time; a team takes consecutive rows, which come through a ring of bulk copies in shared memory, two
 // stages ahead.  A thread has the same columns of each row: the vectors stay in its registers and the vectors' gradients are summed there.  A
 // CTA's sums go to scratch and a second kernel adds them in order (no atomics: the same bits every time).  Row chunks are whole groups, or whole parts
 // of one group.  Rows that are not a multiple of 16 bytes, or too long for the ring, are read straight from global memory.
@@ -182,7 +182,10 @@ template <typename T, int V>
 cudaError_t forward_by(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st)
 {
     const int by = by_of(p);
-    return by == BY_RING ? forward_kind<T, V, BY_RING>(p, layer, ctas, st) : by == BY_PIECES ? forward_kind<T, V, BY_PIECES>(p, layer, ctas, st) : forward_kind<T, V, BY_ELEMENT>(p, layer, ctas, st);
+    if (by == BY_RING) return forward_kind<T, V, BY_RING>(p, layer, ctas, st);
+    if constexpr (V == 4)                    // (up to 8192 columns a ring always fits)
+        if (by == BY_PIECES) return forward_kind<T, V, BY_PIECES>(p, layer, ctas, st);
+    return forward_kind<T, V, BY_ELEMENT>(p, layer, ctas, st);
 }
 template <typename T>
 cudaError_t forward_pieces(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st)

@@ -276,11 +276,12 @@ cudaError_t backward_parts(const NormParams& p, int64_t ctas, cudaStream_t st)
         if (both && !p.f) return run_backward<T, V, BY, LAYER, NT, PRE_ONLY>(p, ctas, st);
     return run_backward<T, V, BY, LAYER, NT, ANY_PARTS>(p, ctas, st);
 }
+// (Up to 4096 columns a ring always fits, and element by element two pieces a thread begin there: the other combinations do not occur.)
 template <typename T, int V, int BY, bool LAYER>
 cudaError_t backward_threads_of(const NormParams& p, int64_t ctas, cudaStream_t st)
 {
-    if constexpr (V == 4) return backward_parts<T, V, BY, LAYER, 512>(p, ctas, st);
-    else if constexpr (V == 1 && BY != BY_ELEMENT) return backward_parts<T, V, BY, LAYER, 256>(p, ctas, st);
+    if constexpr (V == 4 || (V == 2 && BY != BY_RING)) return backward_parts<T, V, BY, LAYER, 512>(p, ctas, st);
+    else if constexpr (V == 1 && BY == BY_RING) return backward_parts<T, V, BY, LAYER, 256>(p, ctas, st);
     else return backward_threads(p.d, p.vec) == 256 ? backward_parts<T, V, BY, LAYER, 256>(p, ctas, st) : backward_parts<T, V, BY, LAYER, 512>(p, ctas, st);
 }
 template <typename T, int V, int BY>
@@ -289,7 +290,10 @@ template <typename T, int V>
 cudaError_t backward_by(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st)
 {
     const int by = by_of(p);
-    return by == BY_RING ? backward_kind<T, V, BY_RING>(p, layer, ctas, st) : by == BY_PIECES ? backward_kind<T, V, BY_PIECES>(p, layer, ctas, st) : backward_kind<T, V, BY_ELEMENT>(p, layer, ctas, st);
+    if (by == BY_RING) return backward_kind<T, V, BY_RING>(p, layer, ctas, st);
+    if constexpr (V > 1)
+        if (by == BY_PIECES) return backward_kind<T, V, BY_PIECES>(p, layer, ctas, st);
+    return backward_kind<T, V, BY_ELEMENT>(p, layer, ctas, st);
 }
 template <typename T>
 cudaError_t backward_pieces(const NormParams& p, bool layer, int64_t ctas, cudaStream_t st)
