@@ -318,3 +318,16 @@ def test_binding_refusals():
     for bad in (x.half(), x[:, ::2], x[0]):
         with pytest.raises(b.SBError):
             b.norm_forward(bad, w)
+
+
+def test_misaligned_vectors_are_refused():
+    """Vectors and their gradients are floats: any other address would be a fault of the kernel's."""
+    b = sb()
+    a, odd, n = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1002), None
+    c = ctypes.byref(b.sb_norm_config(4, 2, 8, 0, 1, 1e-6))
+    for i in (1, 3, 4, 5):                    # w_pre, w_post, gate, scale
+        assert b.sb_norm_forward(c, *[odd if k == i else a for k in range(9)], n) == 1, i
+        assert "misaligned" in b.sb_last_error()
+    for i in (4, 6, 7, 8, 11, 12, 13, 14):    # the same, and their gradients
+        assert b.sb_norm_backward(c, *[odd if k == i else a for k in range(15)], a, 1 << 20, n) == 1, i
+        assert "misaligned" in b.sb_last_error()
