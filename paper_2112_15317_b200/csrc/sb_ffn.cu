@@ -7,6 +7,7 @@
 // kernels (every operand as three bf16 terms on tensor cores, or on CUDA cores where that is faster) with an elementwise kernel between them.
 // Widths that are not multiples of eight: the operands are copied into rows of the next multiple, filled up with zeros, which add nothing to any product, and
 // the results cut out again.  (250 rows, 1023 x 2731, float, backward: 350 us on the CUDA-core kernel for odd widths, 131 so.)
+// (A row with an infinite operand may then be NaN where the unpadded product is infinite: infinity times a zero of the filling.)
 // Roundings in bf16: H, and dG and dU, where they become operands of a product; everything else is rounded once, at the end.
 #include "sb_ffn.h"
 #include "sb_ffn_umma.h"

@@ -1,7 +1,8 @@
 // Gated feed-forward block for few rows (bf16): products whose time is the reading of the weights.
 //
 // The weights are the M side of the MMA (128 of their output columns a CTA) and the rows the N side (16 to 128), so that one token pads to 16 columns
-// and not to 128 rows.  What bounds it: HBM.  A CTA holds a ring of about 100 KB, two CTAs fit an SM, and the reduction is split over a cluster of up to
+// and not to 128 rows.  What bounds it: HBM (one row, 4096 x 8192, forward: 36.6 us, 5.5 TB/s of weights; the rest is launch, set-up and the clusters'
+// sums of two dependent kernels).  A CTA holds a ring of about 100 KB, two CTAs fit an SM, and the reduction is split over a cluster of up to
 // eight CTAs until the machine is full: 100 to 290 CTAs with deep rings keep more bytes in flight than HBM's latency needs, whatever
 // SM they sit on.  The cluster's partial tiles are added through distributed shared memory, in rank order, each CTA finishing its share of the rows: no
 // second kernel, no atomics.  The forward product's tile is 64 gate columns and the 64 up columns that belong to them, so that the activation

@@ -8,8 +8,8 @@ namespace sb {
 
 namespace {
 
-// The vectors' columns of a thread: in registers (eight columns a thread), or in shared memory in the order in which the threads read them (16 columns a
-// thread, whose accumulators take the registers): 16-byte pieces, neighbouring threads' next to each other.  w_pre and scale are the same for every team, and each
+// The vectors' columns of a thread: in registers, or in shared memory in the order in which the threads read them (512 threads with 16 columns
+// each, whose accumulators take their 128 registers): 16-byte pieces, neighbouring threads' next to each other.  w_pre and scale are the same for every team, and each
 // writes them there; a thread only ever reads what it has written itself, or another has with the same values.
 template <int V, bool SHARED> struct Held {
     F2 v[SHARED ? 1 : V][4];
