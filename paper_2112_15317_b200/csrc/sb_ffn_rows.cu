@@ -27,6 +27,9 @@ template <int NT> struct Rw {
     static constexpr int PART = NT * 512;                                                  // one partial tile, float
     static constexpr int BODY = STAGES * STAGE > PART ? STAGES * STAGE : PART;
     static constexpr int SMEM = BODY + 1024 + RW_CTRL;
+    // With this much, no kernel of CTA pairs that takes all 512 columns of tensor memory (136 KB of shared memory or more) fits beside a CTA: clusters
+    // on the same SMs must not wait for each other's columns, each holding some.
+    static_assert(SMEM >= 92 * 1024, "shared memory");
     static constexpr uint32_t TMEM = NT < 32 ? 32 : NT;
 };
 enum { RW_STORE = 0, RW_GLU = 1, RW_GLU_BACK = 2 };
