@@ -342,7 +342,8 @@ const char* sb_partition_last_error(void);
  *   SB_X_GATHER_COLS : shard layer, forward.  src sends its column slice [col0,col1) of layer `layer`'s output for the
  *                      group's rows [row0,row1).
  *   SB_X_REDUCE_COLS : shard layer, backward.  src sends columns [col0,col1) (dst's slice) of its full-width partial
- *                      gradient w.r.t. layer `layer`'s output; dst adds the K partial results in worker order.
+ *                      gradient w.r.t. layer `layer`'s output; dst adds the K partial results in worker order.  Where layer
+ *                      `layer` is kept whole (the split layer above it then has no shard node), dst's slice is the whole width.
  *   SB_X_REDUCE_ROWS : modulo layer, backward.  src sends rows [row0,row1) (dst's examples) of its full-width partial
  *                      gradient w.r.t. the features; dst adds the K partial results in worker order.
  *   SB_X_ALLREDUCE   : the parameters of layer `layer` are held by every worker and trained on its own rows (conv stack):

@@ -17,8 +17,8 @@
 // sb_exchange_plan lists, for N = R workers arranged in R / K MP groups of K = mp workers each [Group MP Extension], every
 // block of every matrix that has to travel between two workers in one synchronous iteration [Modulo Layer and Shard
 // Layer paragraphs and their figures]: the modulo layer's gather of feature rows and the return of gradient rows, the
-// shard layer's gather of column slices and the reduce of gradient column slices -- all of them inside one group --
-// and the two parameter reduces [Distributed Machine Learning: reduce; Implementation]: the conv stack over all N
+// shard layer's gather of column slices and the reduce of gradient column slices (full-width gradients, where a split layer
+// above the modulo layer takes the output of a whole one) -- all of them inside one group -- and the two parameter reduces [Distributed Machine Learning: reduce; Implementation]: the conv stack over all N
 // workers, and each FC shard over the workers that hold the same shard in the other groups.  Worker p belongs to group
 // gid = p / mp and is data replica p and model shard off = p % mp of that group (the lost figure's mapping, taken from
 // the text: the group a worker belongs to, and its offset inside it); with R = K there is a single group, with K = 1
@@ -205,6 +205,16 @@ extern "C" sb_status sb_exchange_plan(const sb_layer* layers, int32_t n, const s
                         bwd_rev.push_back(msg(SB_X_ALLREDUCE_GROUPS, nd.layer, 1, o, -1, 0, 0, lo(o, nd.dimF, mp), lo(o + 1, nd.dimF, mp), nd.dimF));
                 else
                     bwd_rev.push_back(msg(SB_X_ALLREDUCE_GROUPS, nd.layer, 1, -1, -1, 0, 0, 0, nd.dimF, nd.dimF));
+            }
+            // a split layer above the modulo layer whose input is whole on every worker (the layer below is kept whole): no node in front
+            // of it, nothing travels forward; backward, every worker holds a partial full-width gradient of that input, and needs the sum
+            if (k > 0 && fc && nd.shards > 1 && net[k - 1].node == SB_NODE_LAYER) {
+                const int64_t width = net[k - 1].dimF;
+                for (int gid = 0; gid < G; ++gid)
+                    for (int so = 0; so < mp; ++so)
+                        for (int d_o = 0; d_o < mp; ++d_o)
+                            if (so != d_o)
+                                bwd_rev.push_back(msg(SB_X_REDUCE_COLS, nd.layer - 1, 1, gid * mp + so, gid * mp + d_o, gid * Bg, (gid + 1) * Bg, 0, width, width));
             }
         }
     }
