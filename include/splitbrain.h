@@ -417,7 +417,7 @@ sb_status sb_debug_wait_probe(sb_model* m, int32_t limit_ms, void* stream);
 sb_status sb_debug_poison(sb_model* m, void* stream);
 sb_status sb_debug_check_guards(sb_model* m, void* stream, int32_t* n_bad, int64_t* first_bad_offset);
 
-/* Number of kernels the last sb_forward + sb_backward + sb_sgd_step enqueued (host counter). */
+/* Number of kernels the last sb_forward + sb_backward + sb_sgd_step (or sb_adamw_step) enqueued (host counter). */
 sb_status sb_launch_count(const sb_model* m, int64_t* launches);
 
 const char* sb_last_error(void);

@@ -526,17 +526,18 @@ inline int shard_lo(int j, int total, int K) { return (int)(((long)j * total) / 
         }                                                                                         \
     } while (0)
 
-// And for the operators' calls (n launches each), whose kernels report to the model's status word.
-#define O_TRY(tag, flops, bytes, n, expr)                                                         \
+// And for the operators' calls, of as many kernels as they turn out to launch, which report to the model's status word.
+#define O_TRY(tag, flops, bytes, expr)                                                            \
     do {                                                                                          \
         sb_model::Rec rec_{tag, nullptr, nullptr, (double)(flops), (double)(bytes), m->cur_layer}; \
         if (m->profiling) { rec_.e0 = m->next_event(); rec_.e1 = m->next_event();                 \
                             if (rec_.e0) cudaEventRecord(rec_.e0, st); }                          \
         ops_status_of_model() = m->status;                                                        \
+        const int64_t before_ = kernels_launched();                                               \
         const sb_status s_ = (expr);                                                              \
         ops_status_of_model() = nullptr;                                                          \
         if (s_ != SB_OK) return s_;                                                               \
-        m->launches += n;                                                                         \
+        m->launches += kernels_launched() - before_;                                              \
         if (m->profiling && rec_.e1) { cudaEventRecord(rec_.e1, st); m->recs.push_back(rec_); }   \
         if (m->debug_sync) {                                                                      \
             cudaError_t d_ = cudaStreamSynchronize(st);                                           \
@@ -729,10 +730,10 @@ sb_status forward_layer(sb_model* m, int i, cudaStream_t st)
         const void *wgu = wts, *wd = bf ? (const void*)(m->Sm + l.p_w2) : (const void*)(m->Wm + l.p_w2);
         const double act = (double)B * l.in_f * e, hid = (double)B * l.out * e;
         float* st2 = l.blk_stats + (size_t)B * 4;
-        O_TRY("block_norm", 0.0, 2.0 * act, 1, sb_norm_forward(&pre, x, v, nullptr, nullptr, nullptr, nullptr, nullptr, l.blk_n, l.blk_stats, st));
-        O_TRY("block_ffn_fwd", 6.0 * B * l.in_f * (double)l.out, 2.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * e, 2,
+        O_TRY("block_norm", 0.0, 2.0 * act, sb_norm_forward(&pre, x, v, nullptr, nullptr, nullptr, nullptr, nullptr, l.blk_n, l.blk_stats, st));
+        O_TRY("block_ffn_fwd", 6.0 * B * l.in_f * (double)l.out, 2.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * e,
               sb_ffn_forward(&fc, l.blk_n, wgu, wd, l.blk_gu, l.blk_f, m->blk_ws, m->blk_ws_bytes, st));
-        O_TRY("block_norm", 0.0, 3.0 * act, 1, sb_norm_forward(&post, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, l.act, nullptr, st2, st));
+        O_TRY("block_norm", 0.0, 3.0 * act, sb_norm_forward(&post, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, l.act, nullptr, st2, st));
         break;
     }
     case SB_SOFTMAX_XENT: {
@@ -875,12 +876,12 @@ sb_status backward_layer(sb_model* m, int i, cudaStream_t st, int part = SIDE_BO
         const void *wgu = wts, *wd = bf ? (const void*)(m->Sm + l.p_w2) : (const void*)(m->Wm + l.p_w2);
         const double act = (double)B * l.in_f * e, hid = (double)B * l.out * e;
         const float* st2 = l.blk_stats + (size_t)B * 4;
-        O_TRY("block_norm_bwd", 0.0, 5.0 * act, 2, sb_norm_backward(&post, l.dact, nullptr, st2, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, d_below, m->blk_df,
+        O_TRY("block_norm_bwd", 0.0, 5.0 * act, sb_norm_backward(&post, l.dact, nullptr, st2, x, nullptr, l.blk_f, v + l.vec, v + 2 * l.vec, v + 3 * l.vec, d_below, m->blk_df,
                                                                      nullptr, dv + l.vec, dv + 2 * l.vec, dv + 3 * l.vec, m->blk_ws, m->blk_ws_bytes, st));
-        O_TRY("block_ffn_bwd", 12.0 * B * l.in_f * (double)l.out, 3.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * (e + 4.0), 2,
+        O_TRY("block_ffn_bwd", 12.0 * B * l.in_f * (double)l.out, 3.0 * act + 2.0 * hid + 3.0 * l.in_f * (double)l.out * (e + 4.0),
               sb_ffn_backward(&fc, m->blk_df, l.blk_n, l.blk_gu, wgu, wd, m->blk_dn, m->Gm + l.p_w, m->Gm + l.p_w2, m->blk_ws, m->blk_ws_bytes, st));
         // the residual's gradient, so far in d_below, goes through the first norm in place
-        O_TRY("block_norm_bwd", 0.0, 4.0 * act, 2, norm_backward(&pre, d_below, m->blk_dn, l.blk_stats, x, v, nullptr, nullptr, nullptr, nullptr, d_below, nullptr,
+        O_TRY("block_norm_bwd", 0.0, 4.0 * act, norm_backward(&pre, d_below, m->blk_dn, l.blk_stats, x, v, nullptr, nullptr, nullptr, nullptr, d_below, nullptr,
                                                                   dv, nullptr, nullptr, nullptr, m->blk_ws, m->blk_ws_bytes, below_relu, st));
         break;
     }
@@ -1690,7 +1691,7 @@ sb_status sb_adamw_step(sb_model* m, const sb_adamw_hyper* hyper, int64_t step, 
     const sb_adamw_config c{0, 32, SB_DT_F32};
     cudaStream_t st = (cudaStream_t)stream;
     m->cur_layer = -1;
-    O_TRY("adamw", 0.0, (double)m->P * (m->bf16 ? 30.0 : 28.0), 1, sb_adamw_tensors(&t, 1, &c, hyper, step, stream));
+    O_TRY("adamw", 0.0, (double)m->P * (m->bf16 ? 30.0 : 28.0), sb_adamw_tensors(&t, 1, &c, hyper, step, stream));
     m->last_step_launches = m->launches;
     return SB_OK;
 }

@@ -287,6 +287,7 @@ cudaError_t launch_rows(const RowsArgs& a, int tiles, int S, cudaStream_t st)
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    ++kernels_launched();
     return cudaLaunchKernelEx(&cfg, ffn_rows_kernel<NT, EPI>, a);
 }
 template <int EPI>

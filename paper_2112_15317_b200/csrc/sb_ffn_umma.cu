@@ -451,6 +451,7 @@ cudaError_t launch_pair(PairArgs& a, cudaStream_t st)
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    ++kernels_launched();
     return cudaLaunchKernelEx(&cfg, ffn_pair_kernel<EPI, ACT>, a);
 }
 

@@ -55,6 +55,8 @@ inline bool pdl_enabled()
 // Scheduling priority of the calling thread's next launches (0 = least, negative before it): which of the kernels that are ready gets
 // the SMs another one's finished blocks leave.  In a graph it counts where the graph is instantiated with its nodes' priorities.
 inline int& launch_priority() { static thread_local int p = 0; return p; }
+// Kernels that the calling thread has launched (by pdl_launch, and the block's kernels in clusters): what an operator's call consists of depends on its sizes.
+inline int64_t& kernels_launched() { static thread_local int64_t n = 0; return n; }
 template <typename... KArgs, typename... Args>
 inline cudaError_t pdl_launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args)
 {
@@ -75,6 +77,7 @@ inline cudaError_t pdl_launch(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
     }
     cfg.attrs = at;
     cfg.numAttrs = n;
+    ++kernels_launched();
     return cudaLaunchKernelEx(&cfg, kern, KArgs(std::forward<Args>(args))...);
 }
 // Raises a kernel's dynamic shared-memory limit, once per device (the attribute belongs to the device's copy of the function).
