@@ -383,8 +383,9 @@ def norm_backward(dy, dn, stats, x, w_pre=None, f=None, w_post=None, gate=None, 
 
 class AdamW:
     """AdamW over a list of parameters (float, updated in place) with gradients and moments of the caller's: the moments as float tensors, or in
-    8 bits (m: float8_e4m3fn or uint8, v: uint8, and a float scale for each 256 elements of either).  The tensors are looked at once, here;
-    `grads` may be replaced (set_grads).  shadows: bf16 copies of the parameters, refreshed by every step."""
+    8 bits (m: float8_e4m3fn or uint8, v: uint8, and a float scale for each 256 elements of either).  The tensors are looked at once, here, and
+    used where they lie then (their memory is kept); `grads` may be replaced (set_grads).  A step whose parameters have moved since (`p.data = ...`, a
+    storage that was resized) is refused: make a new AdamW then.  shadows: bf16 copies of the parameters, refreshed by every step."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, shadows=None, seed=0):
         import torch
@@ -403,6 +404,8 @@ class AdamW:
         bits = 32 if m_scale is None else 8
         self._list = (sb_adamw_tensor * n)()
         self.cfg = sb_adamw_config(seed, bits, SB_DT_F32)
+        self._params_at = [p.data_ptr() for p in params]
+        self._storages = [t.untyped_storage() for x in (params, m, v, m_scale, v_scale, shadows) if x is not None for t in x if t is not None]
         for i, (e, p) in enumerate(zip(self._list, params)):
             k = p.numel()
             e.n, e.param = k, _dense(f"params[{i}]", p, p.shape, torch.float32, dev)
@@ -430,10 +433,19 @@ class AdamW:
         for e, ptr in zip(self._list, ptrs):         # (all or none)
             e.grad = ptr
         self.cfg.grad_dtype = SB_DT_BF16 if dtype == torch.bfloat16 else SB_DT_F32
-        self._grads = grads
+        self._grads = grads, [g.untyped_storage() for g in grads if g is not None]
+
+    def _check_places(self):
+        # (0.06 us a parameter; all tensors instead would be as much again for each of them: 40 parameters, 9 us on a call of 7)
+        torch, params = self._t[:2]
+        now = list(map(torch.Tensor.data_ptr, params))
+        if now != self._params_at:
+            moved = [tuple(p.shape) for p, a, b in zip(params, now, self._params_at) if a != b]
+            raise SBError(1, f"{len(moved)} of the parameters have moved since this AdamW was made (the first of shape {moved[0]}): make a new one")
 
     def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
         """dev_step (int64) / dev_lr (float32): one-element device tensors to read instead of step / lr, for a step captured into a graph."""
+        self._check_places()
         torch, here, stream = _on_device(self._t[1][0])
         h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _dense("dev_step", dev_step, (1,), torch.int64, self.device),
                            _dense("dev_lr", dev_lr, (1,), torch.float32, self.device))
@@ -442,6 +454,7 @@ class AdamW:
 
     def moments(self):
         """What the 8-bit moments stand for: two lists of bf16 tensors."""
+        self._check_places()
         torch, params = self._t[:2]
         _, here, stream = _on_device(params[0])
         if self._room is None:        # every tensor's place in one buffer, at a multiple of eight elements; the pieces it is cut into, those that are no gaps
