@@ -385,7 +385,8 @@ class AdamW:
     """AdamW over a list of parameters (float, updated in place) with gradients and moments of the caller's: the moments as float tensors, or in
     8 bits (m: float8_e4m3fn or uint8, v: uint8, and a float scale for each 256 elements of either).  The tensors are looked at once, here, and
     used where they lie then (their memory is kept); `grads` may be replaced (set_grads).  A step whose parameters have moved since (`p.data = ...`, a
-    storage that was resized) is refused: make a new AdamW then.  shadows: bf16 copies of the parameters, refreshed by every step."""
+    storage that was resized) is refused: make a new AdamW then.  shadows: bf16 copies of the parameters, refreshed by every step.  What a step writes
+    must not overlap, nor lie in a gradient."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, shadows=None, seed=0):
         import torch
@@ -404,8 +405,9 @@ class AdamW:
         bits = 32 if m_scale is None else 8
         self._list = (sb_adamw_tensor * n)()
         self.cfg = sb_adamw_config(seed, bits, SB_DT_F32)
+        self._written = [t for x in (params, m, v, m_scale, v_scale, shadows) if x is not None for t in x if t is not None]
         self._params_at = [p.data_ptr() for p in params]
-        self._storages = [t.untyped_storage() for x in (params, m, v, m_scale, v_scale, shadows) if x is not None for t in x if t is not None]
+        self._storages = [t.untyped_storage() for t in self._written]
         for i, (e, p) in enumerate(zip(self._list, params)):
             k = p.numel()
             e.n, e.param = k, _dense(f"params[{i}]", p, p.shape, torch.float32, dev)
@@ -418,7 +420,7 @@ class AdamW:
                     setattr(e, name + "_scale", _dense(f"{name}_scale[{i}]", scale[i], (-(-k // 256),), torch.float32, dev))
             if shadows is not None:
                 e.shadow = _dense(f"shadows[{i}]", shadows[i], p.shape, torch.bfloat16, dev)
-        self.device, self._room = dev, None
+        self.device, self._room, self._apart = dev, None, False
         self.set_grads(grads)
 
     def set_grads(self, grads):
@@ -443,9 +445,19 @@ class AdamW:
             moved = [tuple(p.shape) for p, a, b in zip(params, now, self._params_at) if a != b]
             raise SBError(1, f"{len(moved)} of the parameters have moved since this AdamW was made (the first of shape {moved[0]}): make a new one")
 
+    def _check_apart(self):
+        # (once: the addresses do not change)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k) for k, t in enumerate(self._written) if t.numel())
+        for (_, end, i), (begin, _, k) in zip(spans, spans[1:]):
+            if begin < end:
+                raise SBError(1, f"tensors that a step writes overlap: shapes {tuple(self._written[i].shape)} and {tuple(self._written[k].shape)}")
+        self._apart = True
+
     def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
         """dev_step (int64) / dev_lr (float32): one-element device tensors to read instead of step / lr, for a step captured into a graph."""
         self._check_places()
+        if not self._apart:
+            self._check_apart()
         torch, here, stream = _on_device(self._t[1][0])
         h = sb_adamw_hyper(lr, beta1, beta2, eps, weight_decay, _dense("dev_step", dev_step, (1,), torch.int64, self.device),
                            _dense("dev_lr", dev_lr, (1,), torch.float32, self.device))
