@@ -7,7 +7,7 @@
 // kernels (every operand as three bf16 terms on tensor cores, or on CUDA cores where that is faster) with an elementwise kernel between them.
 // Widths that are not multiples of eight: the operands are copied into rows of the next multiple, filled up with zeros, which add nothing to any product, and
 // the results cut out again.  (250 rows, 1023 x 2731, float, backward: 350 us on the CUDA-core kernel for odd widths, 131 so.)
-// (A row with an infinite operand may then be NaN where the unpadded product is infinite: infinity times a zero of the filling.)
+// (H, dG and dU are zero in the filled-up columns whatever comes out there: an infinite operand times their zeros is NaN, which the next product would spread over the row.)
 // Roundings in bf16: H, and dG and dU, where they become operands of a product; everything else is rounded once, at the end.
 #include "sb_ffn.h"
 #include "sb_ffn_umma.h"
@@ -20,18 +20,21 @@ namespace {
 
 constexpr size_t MAX_PART_FLOATS = (size_t)16 << 20;
 
-// H = a(G) * U; widths that are multiples of four, four columns a thread
-__global__ void __launch_bounds__(256) ffn_act_kernel(const float4* gu, float4* h, int64_t rows, int f4, int act)
+// Four columns, those from `live` on as zeros
+__device__ __forceinline__ float4 live_columns(float4 v, int live) { return make_float4(live > 0 ? v.x : 0.f, live > 1 ? v.y : 0.f, live > 2 ? v.z : 0.f, live > 3 ? v.w : 0.f); }
+// H = a(G) * U; widths that are multiples of four, four columns a thread; columns from f_real on are zero
+__global__ void __launch_bounds__(256) ffn_act_kernel(const float4* gu, float4* h, int64_t rows, int f4, int f_real, int act)
 {
     pdl_prologue();
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
         for (int c = blockIdx.y * 256 + threadIdx.x; c < f4; c += gridDim.y * 256) {
             const float4 g = gu[r * 2 * f4 + c], u = gu[r * 2 * f4 + f4 + c];
-            h[r * f4 + c] = make_float4(ffn_act<true>(g.x, act) * u.x, ffn_act<true>(g.y, act) * u.y, ffn_act<true>(g.z, act) * u.z, ffn_act<true>(g.w, act) * u.w);
+            h[r * f4 + c] = live_columns(make_float4(ffn_act<true>(g.x, act) * u.x, ffn_act<true>(g.y, act) * u.y, ffn_act<true>(g.z, act) * u.z, ffn_act<true>(g.w, act) * u.w),
+                                         f_real - 4 * c);
         }
 }
 // dG, dU and H from GU and dH
-__global__ void __launch_bounds__(256) ffn_act_backward_kernel(const float4* dh, const float4* gu, float4* dgu, float4* h, int64_t rows, int f4, int act)
+__global__ void __launch_bounds__(256) ffn_act_backward_kernel(const float4* dh, const float4* gu, float4* dgu, float4* h, int64_t rows, int f4, int f_real, int act)
 {
     pdl_prologue();
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
@@ -41,16 +44,17 @@ __global__ void __launch_bounds__(256) ffn_act_backward_kernel(const float4* dh,
             float4 da, a;
             a.x = ffn_act_grad<true>(g.x, act, da.x); a.y = ffn_act_grad<true>(g.y, act, da.y);
             a.z = ffn_act_grad<true>(g.z, act, da.z); a.w = ffn_act_grad<true>(g.w, act, da.w);
-            dgu[at] = make_float4(d.x * u.x * da.x, d.y * u.y * da.y, d.z * u.z * da.z, d.w * u.w * da.w);
-            dgu[at + f4] = make_float4(d.x * a.x, d.y * a.y, d.z * a.z, d.w * a.w);
-            h[r * f4 + c] = make_float4(a.x * u.x, a.y * u.y, a.z * u.z, a.w * u.w);
+            const int live = f_real - 4 * c;
+            dgu[at] = live_columns(make_float4(d.x * u.x * da.x, d.y * u.y * da.y, d.z * u.z * da.z, d.w * u.w * da.w), live);
+            dgu[at + f4] = live_columns(make_float4(d.x * a.x, d.y * a.y, d.z * a.z, d.w * a.w), live);
+            h[r * f4 + c] = live_columns(make_float4(a.x * u.x, a.y * u.y, a.z * u.z, a.w * u.w), live);
         }
 }
 
 // Matrices of one element size copied into others with rows of another length; what the source does not have is zero.  A block takes pieces of eight
 // rows x 256 columns of any of them, a thread one column: eight loads under way, whatever the shapes.
 struct CopyOne { const void* src; void* dst; int64_t src_rows, src_cols; int src_ld; int64_t rows, cols; int ld; int64_t first; int across; };      // pieces before it, pieces across
-struct CopyArgs { CopyOne m[7]; int count; int64_t pieces; };
+struct CopyArgs { CopyOne m[10]; int count; int64_t pieces; };
 template <typename T>
 __global__ void __launch_bounds__(256) ffn_copy_kernel(const __grid_constant__ CopyArgs a)
 {
@@ -153,7 +157,7 @@ dim3 act_grid(const sb_ffn_config* c)
     return dim3((unsigned)std::min<int64_t>(c->rows, 148 * 8), (unsigned)std::min(cols, 16));
 }
 
-sb_status float_forward(const sb_ffn_config* c, const float* x, const float* w_gu, const float* w_down, float* gu, float* y, void* ws, cudaStream_t st)
+sb_status float_forward(const sb_ffn_config* c, const float* x, const float* w_gu, const float* w_down, float* gu, float* y, void* ws, int f_real, cudaStream_t st)
 {
     Carve k{(char*)ws};
     const FloatForward w = carve_forward(k, c);
@@ -162,7 +166,7 @@ sb_status float_forward(const sb_ffn_config* c, const float* x, const float* w_g
     ContractArgs a = contract_of(CMODE_FWD, c, c->d, 2 * c->f, w.part);
     a.act = x; a.wt = w_gu; a.bias = w.zero; a.out = g;
     F_TRY(launch_contract(a, false, st));
-    F_TRY(pdl_launch(ffn_act_kernel, act_grid(c), dim3(256), 0, st, (const float4*)g, (float4*)w.h, c->rows, c->f / 4, c->act));
+    F_TRY(pdl_launch(ffn_act_kernel, act_grid(c), dim3(256), 0, st, (const float4*)g, (float4*)w.h, c->rows, c->f / 4, f_real, c->act));
     ContractArgs b = contract_of(CMODE_FWD, c, c->f, c->d, w.part);
     b.act = w.h; b.wt = w_down; b.bias = w.zero; b.out = y;
     F_TRY(launch_contract(b, false, st));
@@ -185,14 +189,14 @@ sb_status weight_gradient(const sb_ffn_config* c, const float* act, const float*
 }
 
 sb_status float_backward(const sb_ffn_config* c, const float* dy, const float* x, const float* gu, const float* w_gu, const float* w_down, float* dx, float* dw_gu,
-                         float* dw_down, void* ws, cudaStream_t st)
+                         float* dw_down, void* ws, int f_real, cudaStream_t st)
 {
     Carve k{(char*)ws};
     const FloatBackward w = carve_backward(k, c);
     ContractArgs a = contract_of(CMODE_DGRAD, c, c->f, c->d, w.part);
     a.wt = w_down; a.dy = dy; a.out = w.dh;
     F_TRY(launch_contract(a, false, st));
-    F_TRY(pdl_launch(ffn_act_backward_kernel, act_grid(c), dim3(256), 0, st, (const float4*)w.dh, (const float4*)gu, (float4*)w.dgu, (float4*)w.h, c->rows, c->f / 4, c->act));
+    F_TRY(pdl_launch(ffn_act_backward_kernel, act_grid(c), dim3(256), 0, st, (const float4*)w.dh, (const float4*)gu, (float4*)w.dgu, (float4*)w.h, c->rows, c->f / 4, f_real, c->act));
     if (dx) {
         ContractArgs b = contract_of(CMODE_DGRAD, c, c->d, 2 * c->f, w.part);
         b.wt = w_gu; b.dy = w.dgu; b.out = dx;
@@ -211,16 +215,16 @@ size_t even_bytes(const sb_ffn_config* c, bool backward)
     if (backward) carve_backward(k, c); else carve_forward(k, c);
     return k.off;
 }
-sb_status even_forward(const sb_ffn_config* c, const void* x, const void* w_gu, const void* w_down, void* gu, void* y, void* ws, cudaStream_t st)
+sb_status even_forward(const sb_ffn_config* c, const void* x, const void* w_gu, const void* w_down, void* gu, void* y, void* ws, int f_real, cudaStream_t st)
 {
-    if (ffn_umma_ok(c)) return ffn_umma_forward(c, x, w_gu, w_down, gu, y, ws, st);
-    return float_forward(c, (const float*)x, (const float*)w_gu, (const float*)w_down, (float*)gu, (float*)y, ws, st);
+    if (ffn_umma_ok(c)) return ffn_umma_forward(c, x, w_gu, w_down, gu, y, ws, f_real, st);
+    return float_forward(c, (const float*)x, (const float*)w_gu, (const float*)w_down, (float*)gu, (float*)y, ws, f_real, st);
 }
 sb_status even_backward(const sb_ffn_config* c, const void* dy, const void* x, const void* gu, const void* w_gu, const void* w_down, void* dx, void* dw_gu,
-                        void* dw_down, void* ws, cudaStream_t st)
+                        void* dw_down, void* ws, int f_real, cudaStream_t st)
 {
-    if (ffn_umma_ok(c)) return ffn_umma_backward(c, dy, x, gu, w_gu, w_down, dx, dw_gu, dw_down, ws, st);
-    return float_backward(c, (const float*)dy, (const float*)x, (const float*)gu, (const float*)w_gu, (const float*)w_down, (float*)dx, (float*)dw_gu, (float*)dw_down, ws, st);
+    if (ffn_umma_ok(c)) return ffn_umma_backward(c, dy, x, gu, w_gu, w_down, dx, dw_gu, dw_down, ws, f_real, st);
+    return float_backward(c, (const float*)dy, (const float*)x, (const float*)gu, (const float*)w_gu, (const float*)w_down, (float*)dx, (float*)dw_gu, (float*)dw_down, ws, f_real, st);
 }
 
 // ---- any width ----
@@ -254,6 +258,16 @@ void copy_of(CopyArgs& a, const void* src, int64_t rows, int64_t cols, int64_t s
     a.m[a.count++] = CopyOne{src, dst, rows, cols, (int)src_ld, to_rows, to_cols, (int)ld, a.pieces, across};
     a.pieces += (to_rows + 7) / 8 * across;
 }
+// zeros into what is H's filling in bf16, [dG dU]'s too in the backward pass (float: the activation kernels write them)
+void clear_filling(CopyArgs& a, const sb_ffn_config* c, const sb_ffn_config* p, void* inner, bool backward)
+{
+    if (c->precision != SB_BF16 || c->f == p->f) return;
+    const int64_t fill = p->f - c->f;
+    copy_of(a, nullptr, 0, 0, 0, ffn_umma_h(p, inner) + c->f, c->rows, fill, p->f);
+    if (!backward) return;
+    copy_of(a, nullptr, 0, 0, 0, ffn_umma_dgu(p, inner) + c->f, c->rows, fill, 2 * p->f);
+    copy_of(a, nullptr, 0, 0, 0, ffn_umma_dgu(p, inner) + p->f + c->f, c->rows, fill, 2 * p->f);
+}
 cudaError_t launch_copies(const CopyArgs& a, size_t e, cudaStream_t st)
 {
     const dim3 grid((unsigned)std::min<int64_t>(a.pieces, 148 * 32));
@@ -274,8 +288,9 @@ sb_status odd_forward(const sb_ffn_config* c, const void* x, const void* w_gu, c
     copy_of(in, w_gu, F, D, D, w.w_gu, F2, D2, D2);
     copy_of(in, behind(w_gu, F * D, e), F, D, D, behind((void*)w.w_gu, F2 * D2, e), F2, D2, D2);
     copy_of(in, w_down, D, F, F, w.w_down, D2, F2, F2);
+    clear_filling(in, c, &p, w.inner, false);
     F_TRY(launch_copies(in, e, st));
-    S_TRY(even_forward(&p, w.x, w.w_gu, w.w_down, gu ? w.gu : nullptr, w.y, w.inner, st));
+    S_TRY(even_forward(&p, w.x, w.w_gu, w.w_down, gu ? w.gu : nullptr, w.y, w.inner, c->f, st));
     copy_of(out, w.y, R, D, D2, y, R, D, D);
     if (gu) {
         copy_of(out, w.gu, R, F, 2 * F2, gu, R, F, 2 * F);
@@ -300,8 +315,9 @@ sb_status odd_backward(const sb_ffn_config* c, const void* dy, const void* x, co
     copy_of(in, w_gu, F, D, D, w.w_gu, F2, D2, D2);
     copy_of(in, behind(w_gu, F * D, e), F, D, D, behind((void*)w.w_gu, F2 * D2, e), F2, D2, D2);
     copy_of(in, w_down, D, F, F, w.w_down, D2, F2, F2);
+    clear_filling(in, c, &p, w.inner, true);
     F_TRY(launch_copies(in, e, st));
-    S_TRY(even_backward(&p, w.dy, w.x, w.gu, w.w_gu, w.w_down, dx ? w.y : nullptr, dw_gu ? w.dw_gu : nullptr, dw_down ? w.dw_down : nullptr, w.inner, st));
+    S_TRY(even_backward(&p, w.dy, w.x, w.gu, w.w_gu, w.w_down, dx ? w.y : nullptr, dw_gu ? w.dw_gu : nullptr, dw_down ? w.dw_down : nullptr, w.inner, c->f, st));
     CopyArgs& g = ge == e ? out : grads;
     if (dx) copy_of(out, w.y, R, D, D2, dx, R, D, D);
     if (dw_gu) {
@@ -386,7 +402,7 @@ sb_status sb_ffn_forward(const sb_ffn_config* c, const void* x, const void* w_ga
     if (!x || !w_gate_up || !w_down || !y) return set_error(SB_ERR_INVALID_ARG, "null matrix");
     if (!aligned16(x) || !aligned16(w_gate_up) || !aligned16(w_down) || !aligned16(gu) || !aligned16(y)) return set_error(SB_ERR_INVALID_ARG, "every matrix must be 16-byte aligned");
     if (!ops_status()) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
-    return even(c) ? even_forward(c, x, w_gate_up, w_down, gu, y, ws, (cudaStream_t)stream) : odd_forward(c, x, w_gate_up, w_down, gu, y, ws, (cudaStream_t)stream);
+    return even(c) ? even_forward(c, x, w_gate_up, w_down, gu, y, ws, c->f, (cudaStream_t)stream) : odd_forward(c, x, w_gate_up, w_down, gu, y, ws, (cudaStream_t)stream);
 }
 
 sb_status sb_ffn_backward(const sb_ffn_config* c, const void* dy, const void* x, const void* gu, const void* w_gate_up, const void* w_down, void* dx,
@@ -404,7 +420,7 @@ sb_status sb_ffn_backward(const sb_ffn_config* c, const void* dy, const void* x,
     }
     if (!dy || !x || !gu || !w_gate_up || !w_down) return set_error(SB_ERR_INVALID_ARG, "null matrix");
     if (!ops_status()) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
-    return even(c) ? even_backward(c, dy, x, gu, w_gate_up, w_down, dx, dw_gate_up, dw_down, ws, (cudaStream_t)stream)
+    return even(c) ? even_backward(c, dy, x, gu, w_gate_up, w_down, dx, dw_gate_up, dw_down, ws, c->f, (cudaStream_t)stream)
                    : odd_backward(c, dy, x, gu, w_gate_up, w_down, dx, dw_gate_up, dw_down, ws, (cudaStream_t)stream);
 }
 

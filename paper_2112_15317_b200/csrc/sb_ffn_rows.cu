@@ -39,6 +39,7 @@ struct alignas(64) RowsArgs {
     int a_mn;                  // weights as they lie: 0 = reduction along a row, 1 = down a column
     int w_split;               // RW_GLU: from a gate row to its up row
     int rows, m, chunks, early, act;
+    int live;                  // RW_GLU, RW_GLU_BACK: H's columns from there on are zero
     const __nv_bfloat16* kept; // RW_GLU_BACK: GU
     __nv_bfloat16 *out, *gu;   // RW_STORE: [rows, m]; RW_GLU: H and (or nullptr) GU; RW_GLU_BACK: H and dG, dU
     uint32_t* status;
@@ -48,10 +49,10 @@ __device__ __forceinline__ void ld_cluster_f32x4(uint32_t caddr, float* v)
 {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(caddr) : "memory");
 }
-__device__ __forceinline__ void store_bf16x4(__nv_bfloat16* p, const float (&v)[4])
+__device__ __forceinline__ void store_bf16x4(__nv_bfloat16* p, const float (&v)[4], uint2 keep = make_uint2(~0u, ~0u))
 {
     const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-    *(uint2*)p = make_uint2(*(const uint32_t*)&a, *(const uint32_t*)&b);
+    *(uint2*)p = make_uint2(*(const uint32_t*)&a & keep.x, *(const uint32_t*)&b & keep.y);
 }
 // (read-only in this kernel: such loads may go ahead of earlier stores)
 __device__ __forceinline__ void load_bf16x4(const __nv_bfloat16* p, float (&v)[4])
@@ -193,6 +194,9 @@ ffn_rows_kernel(const __grid_constant__ RowsArgs a)
                 }
         };
         const int last = min(NT, a.rows - t0);
+        // (bits of this thread's columns that are no filling: selects in the loop took 2 us of 87, backward, 4000 x 512 x 1368)
+        const int live = a.live - col;
+        const uint2 keep = make_uint2(live > 1 ? ~0u : live > 0 ? 0xffffu : 0u, live > 3 ? ~0u : live > 2 ? 0xffffu : 0u);
         if (col < a.m) {
 #pragma unroll 4
             for (int tok = rank + S * (e / LANES); tok < last; tok += S * AT_ONCE) {
@@ -207,7 +211,7 @@ ffn_rows_kernel(const __grid_constant__ RowsArgs a)
                     sum(tok, 64 + part_col, up);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) h[j] = ffn_act<false>(v[j], a.act) * up[j];
-                    store_bf16x4(a.out + row * a.m + col, h);
+                    store_bf16x4(a.out + row * a.m + col, h, keep);
                     if (a.gu) { store_bf16x4(a.gu + at, v); store_bf16x4(a.gu + at + a.m, up); }
                 } else {
                     float g[4], up[4], dg[4], du[4], h[4];
@@ -222,9 +226,9 @@ ffn_rows_kernel(const __grid_constant__ RowsArgs a)
                         du[j] = v[j] * act;
                         h[j] = act * up[j];
                     }
-                    store_bf16x4(a.gu + at, dg);
-                    store_bf16x4(a.gu + at + a.m, du);
-                    store_bf16x4(a.out + row * a.m + col, h);
+                    store_bf16x4(a.gu + at, dg, keep);
+                    store_bf16x4(a.gu + at + a.m, du, keep);
+                    store_bf16x4(a.out + row * a.m + col, h, keep);
                 }
             }
         }
@@ -313,10 +317,10 @@ sb_status map_failed() { return set_error(SB_ERR_CUDA, "ffn: %s", umma_last_erro
 
 double ffn_rows_us(int64_t rows, int tiles, int chunks, int mn) { return rows_plan(rows, tiles, chunks, mn).us; }
 
-sb_status ffn_rows_glu(const sb_ffn_config* c, const void* x, const void* w_gu, void* gu, __nv_bfloat16* h, cudaStream_t st)
+sb_status ffn_rows_glu(const sb_ffn_config* c, const void* x, const void* w_gu, void* gu, __nv_bfloat16* h, int f_real, cudaStream_t st)
 {
     RowsArgs a{};
-    a.rows = (int)c->rows; a.m = c->f; a.w_split = c->f; a.act = c->act; a.out = h; a.gu = (__nv_bfloat16*)gu;
+    a.rows = (int)c->rows; a.m = c->f; a.live = f_real; a.w_split = c->f; a.act = c->act; a.out = h; a.gu = (__nv_bfloat16*)gu;
     if (!weights(a, w_gu, 2 * (int64_t)c->f, c->d, 0)) return map_failed();
     return launch_epi<RW_GLU>(a, x, c->d, cdiv(c->f, 64), st);
 }
@@ -327,10 +331,10 @@ sb_status ffn_rows_down(const sb_ffn_config* c, const __nv_bfloat16* h, const vo
     if (!weights(a, w_down, c->d, c->f, 0)) return map_failed();
     return launch_epi<RW_STORE>(a, h, c->f, cdiv(c->d, 128), st);
 }
-sb_status ffn_rows_glu_back(const sb_ffn_config* c, const void* dy, const void* gu, const void* w_down, __nv_bfloat16* dgu, __nv_bfloat16* h, cudaStream_t st)
+sb_status ffn_rows_glu_back(const sb_ffn_config* c, const void* dy, const void* gu, const void* w_down, __nv_bfloat16* dgu, __nv_bfloat16* h, int f_real, cudaStream_t st)
 {
     RowsArgs a{};
-    a.rows = (int)c->rows; a.m = c->f; a.act = c->act; a.kept = (const __nv_bfloat16*)gu; a.gu = dgu; a.out = h;
+    a.rows = (int)c->rows; a.m = c->f; a.live = f_real; a.act = c->act; a.kept = (const __nv_bfloat16*)gu; a.gu = dgu; a.out = h;
     if (!weights(a, w_down, c->d, c->f, 1)) return map_failed();
     return launch_epi<RW_GLU_BACK>(a, dy, c->d, cdiv(c->f, 128), st);
 }

@@ -493,12 +493,15 @@ static bool on_rows(int64_t rows, int row_tiles, int mn, const PairProblem& p, b
 
 bool ffn_umma_ok(const sb_ffn_config* c) { return c->precision == SB_BF16 && c->d % 8 == 0 && c->f % 8 == 0; }
 
+__nv_bfloat16* ffn_umma_h(const sb_ffn_config*, void* ws) { return (__nv_bfloat16*)ws; }
+__nv_bfloat16* ffn_umma_dgu(const sb_ffn_config* c, void* ws) { return (__nv_bfloat16*)((char*)ws + h_bytes(c)); }
 size_t ffn_umma_bytes(const sb_ffn_config* c, bool backward) { return backward ? 3 * h_bytes(c) : h_bytes(c); }
 
-sb_status ffn_umma_forward(const sb_ffn_config* c, const void* x, const void* w_gu, const void* w_down, void* gu, void* y, void* ws, cudaStream_t st)
+sb_status ffn_umma_forward(const sb_ffn_config* c, const void* x, const void* w_gu, const void* w_down, void* gu, void* y, void* ws, int f_real,
+                           cudaStream_t st)
 {
     const int64_t R = c->rows, D = c->d, F = c->f;
-    __nv_bfloat16* h = (__nv_bfloat16*)ws;
+    __nv_bfloat16* h = ffn_umma_h(c, ws);
     static thread_local PairArgs a;
     a = PairArgs{};
     a.count = 1; a.save = gu != nullptr;
@@ -507,9 +510,9 @@ sb_status ffn_umma_forward(const sb_ffn_config* c, const void* x, const void* w_
     a.p[0].n_tiles = cdiv(F, 128);
     a.p[0].units = a.p[0].m_tiles * a.p[0].n_tiles;
     sb_status s = SB_OK;
-    if (on_rows(R, cdiv(F, 64), 0, a.p[0], false)) s = ffn_rows_glu(c, x, w_gu, gu, h, st);
+    if (on_rows(R, cdiv(F, 64), 0, a.p[0], false)) s = ffn_rows_glu(c, x, w_gu, gu, h, f_real, st);
     else {
-        bool ok = operand(&a.a[0], x, R, D, 0) && operand(&a.b[0], w_gu, 2 * F, D, 0) && umma_map_rows(&a.c[0], h, (long)R, (long)F, (long)F, 128);
+        bool ok = operand(&a.a[0], x, R, D, 0) && operand(&a.b[0], w_gu, 2 * F, D, 0) && umma_map_rows(&a.c[0], h, (long)R, f_real, (long)F, 128);
         if (ok && gu) ok = umma_map_rows(&a.c[1], gu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[2], (const __nv_bfloat16*)gu + F, (long)R, (long)F, (long)(2 * F), 128);
         if (!ok) return map_failed();
         s = launched(launch_pair_act<EPI_GLU>(a, c->act, st));
@@ -524,23 +527,22 @@ sb_status ffn_umma_forward(const sb_ffn_config* c, const void* x, const void* w_
 }
 
 sb_status ffn_umma_backward(const sb_ffn_config* c, const void* dy, const void* x, const void* gu, const void* w_gu, const void* w_down, void* dx, void* dw_gu,
-                            void* dw_down, void* ws, cudaStream_t st)
+                            void* dw_down, void* ws, int f_real, cudaStream_t st)
 {
     const int64_t R = c->rows, D = c->d, F = c->f;
-    __nv_bfloat16* h = (__nv_bfloat16*)ws;
-    __nv_bfloat16* dgu = (__nv_bfloat16*)((char*)ws + h_bytes(c));
+    __nv_bfloat16 *h = ffn_umma_h(c, ws), *dgu = ffn_umma_dgu(c, ws);
     const __nv_bfloat16* kept = (const __nv_bfloat16*)gu;
     static thread_local PairArgs a;
     a = PairArgs{};
     a.count = 1;
     a.p[0] = problem(R, F, D, 0, 1);
     sb_status s = SB_OK;
-    if (on_rows(R, cdiv(F, 128), 1, a.p[0], true)) s = ffn_rows_glu_back(c, dy, gu, w_down, dgu, h, st);
+    if (on_rows(R, cdiv(F, 128), 1, a.p[0], true)) s = ffn_rows_glu_back(c, dy, gu, w_down, dgu, h, f_real, st);
     else {
         bool ok = operand(&a.a[0], dy, R, D, 0) && operand(&a.b[0], w_down, D, F, 1);
         ok = ok && umma_map_rows(&a.g, kept, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.u, kept + F, (long)R, (long)F, (long)(2 * F), 128);
-        ok = ok && umma_map_rows(&a.c[0], dgu, (long)R, (long)F, (long)(2 * F), 128) && umma_map_rows(&a.c[1], dgu + F, (long)R, (long)F, (long)(2 * F), 128) &&
-             umma_map_rows(&a.c[2], h, (long)R, (long)F, (long)F, 128);
+        ok = ok && umma_map_rows(&a.c[0], dgu, (long)R, f_real, (long)(2 * F), 128) && umma_map_rows(&a.c[1], dgu + F, (long)R, f_real, (long)(2 * F), 128) &&
+             umma_map_rows(&a.c[2], h, (long)R, f_real, (long)F, 128);
         if (!ok) return map_failed();
         s = launched(launch_pair_act<EPI_GLU_BACK>(a, c->act, st));
     }
