@@ -52,7 +52,7 @@ norm_forward_kernel(const NormParams p)
             for (int j = 0; j < 4; ++j) q[c][j] = a[j] * b[j];
         }
     };
-    for (int64_t t = (int64_t)blockIdx.x * p.teams + team_id; t < p.turns; t += (int64_t)gridDim.x * p.teams) {
+    for (int64_t t = first_turn(p, team_id); t < p.turns; t += (int64_t)gridDim.x * p.teams) {
         int64_t first, end;
         turn_rows(p, t, first, end);
         const int rows = (int)(end - first), per = BY == BY_RING ? p.stage_rows : 1;
@@ -259,7 +259,8 @@ sb_status norm_backward(const sb_norm_config* c, const void* dy, const void* dn,
     const Turns& t = g.turns;
     p.vec = vec;
     p.dy = dy; p.dn = dn; p.dx = dx; p.df = df; p.stats = (float*)stats; p.relu_x = relu_x;
-    p.chunk = t.chunk; p.turns = t.turns; p.chunks_per_group = t.per_group; p.team = g.team; p.teams = g.teams;
+    spread(p, g);
+    p.chunks_per_group = t.per_group;
     float* part = (float*)ws;
     float* gate_part = part + ((size_t)g.ctas * 3 * c->d + 15) / 16 * 16;
     p.part = want ? part : nullptr;
@@ -301,7 +302,7 @@ sb_status sb_norm_forward(const sb_norm_config* c, const void* x, const float* w
     const bool vec = vec_ok(c->d, x, f, y, n, w_pre, w_post, gate, scale);
     const Grid g = grid_of(c, false, vec);
     p.vec = vec;
-    p.chunk = g.turns.chunk; p.turns = g.turns.turns; p.team = g.team; p.teams = g.teams;
+    spread(p, g);
     p.status = ops_status();
     if (!p.status) return set_error(SB_ERR_CUDA, "the status word has no address on this device");
     // (two CTAs an SM where a warp holds a row)

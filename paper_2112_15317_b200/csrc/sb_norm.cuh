@@ -22,6 +22,7 @@ struct NormParams {
     int chunks_per_group;         // > 1: a group's rows fall to that many turns (chunk of them each, the last one fewer)
     int64_t turns;
     int team, teams;              // warps of a team, teams of a CTA
+    int each, extra;              // teams of a CTA that have turns: one more in the first `extra` CTAs
     int stages, stage_rows, stage_bytes;     // ring of a team (stages = 0: none)
     int vec;                      // 16-byte accesses throughout
     int arrays;                   // row arrays in it
@@ -204,6 +205,14 @@ __device__ __forceinline__ void turn_rows(const NormParams& p, int64_t t, int64_
     }
 }
 
+// A team's first turn (p.turns: none): neighbouring turns to the teams of a CTA, and where there are not enough for all teams, as many to each CTA.  (Filling
+// CTA after CTA: 4000 x 1024, float, a gate row for each row, forward 14.5 us instead of 13.)
+__device__ __forceinline__ int64_t first_turn(const NormParams& p, int team_id)
+{
+    const int b = (int)blockIdx.x, n = p.each + (b < p.extra ? 1 : 0);
+    return team_id < n ? (int64_t)(b * p.each + min(b, p.extra) + team_id) : p.turns;
+}
+
 // A team's ring over the rows of one turn.  A stage holds `stage_rows` rows of x, f, dy, dn, the gate and the stats (those that there are), one array after the
 // other.  The thread that fills it refills a slot when the team has moved on from it: each row ends with a barrier behind its last read.
 struct Ring {
@@ -322,9 +331,16 @@ inline Grid grid_of(const sb_norm_config* c, bool backward, bool vec)
     if (room / (2 * row) >= 1 && (size_t)g.teams > room / (2 * row)) g.teams = (int)(room / (2 * row));
     const int64_t most = two ? 296 : 148;
     g.turns = turns_of(c->rows, backward ? c->groups : 0, most * g.teams);
-    // few turns: one a CTA rather than several teams of few CTAs
+    // few turns: one a CTA rather than several teams of few CTAs (see spread)
     g.ctas = g.turns.turns < most ? g.turns.turns : most;
     return g;
+}
+inline void spread(NormParams& p, const Grid& g)
+{
+    p.team = g.team; p.teams = g.teams; p.turns = g.turns.turns; p.chunk = g.turns.chunk;
+    const bool few = p.turns < g.ctas * g.teams;
+    p.each = few ? (int)(p.turns / g.ctas) : g.teams;
+    p.extra = few ? (int)(p.turns % g.ctas) : 0;
 }
 inline size_t part_floats(const sb_norm_config* c)
 {

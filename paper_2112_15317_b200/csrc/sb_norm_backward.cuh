@@ -97,7 +97,7 @@ norm_backward_kernel(const NormParams p)
                 if (out) put_vector<T, BY>(out, w, c, d, b);
             }
         };
-        for (int64_t t = (int64_t)blockIdx.x * p.teams + team_id; t < p.turns; t += (int64_t)gridDim.x * p.teams) {
+        for (int64_t t = first_turn(p, team_id); t < p.turns; t += (int64_t)gridDim.x * p.teams) {
             int64_t first, end;
             turn_rows(p, t, first, end);
             const int rows = (int)(end - first), per = BY == BY_RING ? p.stage_rows : 1;
