@@ -327,7 +327,8 @@ inline Grid grid_of(const sb_norm_config* c, bool backward, bool vec)
     const bool two = pieces == 1;          // CTAs on an SM
     // (as many as have two stages of a row each in shared memory, where that leaves any)
     const size_t row = (size_t)c->d * (c->precision == SB_BF16 ? 2 : 4) * (backward ? 4 : 2);
-    const size_t room = (size_t)RING_LIMIT / (two ? 2 : 1) - (backward && warps == 16 && pieces == 2 ? 4096 * (size_t)g.team * 8 : 0);
+    // (backward with 16 warps and two pieces, the vectors take a part of it (see vector_bytes), but a row fills more than half of the warps: one team as it is)
+    const size_t room = (size_t)RING_LIMIT / (two ? 2 : 1);
     if (room / (2 * row) >= 1 && (size_t)g.teams > room / (2 * row)) g.teams = (int)(room / (2 * row));
     const int64_t most = two ? 296 : 148;
     g.turns = turns_of(c->rows, backward ? c->groups : 0, most * g.teams);
