@@ -529,6 +529,7 @@ sb_status sb_norm_backward(const sb_norm_config* cfg, const void* dy, const void
  * One AdamW step over a list of tensors, in one kernel for up to 350 of them:
  *   m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2;  p <- (1 - lr wd) p - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
  * list (HOST): param float; grad float or bfloat16 (config); shadow: bfloat16 copy of the parameter to refresh, or NULL; n elements.
+ * Every operation is rounded to float; with 8-bit states the root and the quotient of p's step are approximations (2^-21 of the step).
  * state_bits 32: m and v float, scales unused.  state_bits 8: m and v one byte per element, m_scale and v_scale one float per 256
  * consecutive elements (the last block may be shorter), each a power of two:
  *   m = e4m3(code) * m_scale, rounded to nearest even;  v = u(code) * v_scale, u = five bits of exponent (bias 30; 0: subnormal) and three of

@@ -334,8 +334,9 @@ adamw_kernel(const __grid_constant__ AdamwArgs<N> a)
             const float g = at.g.at(j);
             m[j] = __fadd_rn(__fmul_rn(a.b1, m[j]), __fmul_rn(a.c1, g));
             v[j] = __fadd_rn(__fmul_rn(a.b2, v[j]), __fmul_rn(__fmul_rn(a.c2, g), g));
-            // (the step by the approximations of root and quotient: 2^-21 of a step, which is a small part of p)
-            p[j] = p[j] * decay - rate * __fdividef(m[j], root(v[j]) * rs2 + a.eps);
+            // (8 bits: the step by the approximations of root and quotient, 2^-21 of it, where the moments' codes leave 2^-5.  138 M parameters without a copy,
+            // float gradients: 395 us, 423 with the exact ones.  Float moments: exact, 599 us, 596 with the approximations.)
+            p[j] = p[j] * decay - rate * (BITS == 32 ? __fdiv_rn(m[j], __fsqrt_rn(v[j]) * rs2 + a.eps) : __fdividef(m[j], root(v[j]) * rs2 + a.eps));
         }
         store8(e.p, i, n, vec, p);
         if (e.shadow) store8(e.shadow, i, n, vec, p);
