@@ -406,7 +406,7 @@ class AdamW:
         self._list = (sb_adamw_tensor * n)()
         self.cfg = sb_adamw_config(seed, bits, SB_DT_F32)
         self._written = [t for x in (params, m, v, m_scale, v_scale, shadows) if x is not None for t in x if t is not None]
-        self._params_at = [p.data_ptr() for p in params]
+        self._address_of, self._params_at = torch.Tensor.data_ptr, [p.data_ptr() for p in params]
         self._storages = [t.untyped_storage() for t in self._written]
         for i, (e, p) in enumerate(zip(self._list, params)):
             k = p.numel()
@@ -437,13 +437,10 @@ class AdamW:
         self.cfg.grad_dtype = SB_DT_BF16 if dtype == torch.bfloat16 else SB_DT_F32
         self._grads = grads, [g.untyped_storage() for g in grads if g is not None]
 
-    def _check_places(self):
-        # (0.06 us a parameter; all tensors instead would be as much again for each of them: 40 parameters, 9 us on a call of 7)
-        torch, params = self._t[:2]
-        now = list(map(torch.Tensor.data_ptr, params))
-        if now != self._params_at:
-            moved = [tuple(p.shape) for p, a, b in zip(params, now, self._params_at) if a != b]
-            raise SBError(1, f"{len(moved)} of the parameters have moved since this AdamW was made (the first of shape {moved[0]}): make a new one")
+    # A step compares the parameters' addresses (0.06 us each; those of all tensors would be as much again for every one: 40 parameters, 9 us on a call of 7).
+    def _refuse_moved(self, now):
+        moved = [tuple(p.shape) for p, a, b in zip(self._t[1], now, self._params_at) if a != b]
+        raise SBError(1, f"{len(moved)} of the parameters have moved since this AdamW was made (the first of shape {moved[0]}): make a new one")
 
     def _check_apart(self):
         # (once: the addresses do not change)
@@ -455,7 +452,9 @@ class AdamW:
 
     def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, dev_step=None, dev_lr=None):
         """dev_step (int64) / dev_lr (float32): one-element device tensors to read instead of step / lr, for a step captured into a graph."""
-        self._check_places()
+        now = list(map(self._address_of, self._t[1]))
+        if now != self._params_at:
+            self._refuse_moved(now)
         if not self._apart:
             self._check_apart()
         torch, here, stream = _on_device(self._t[1][0])
@@ -466,8 +465,10 @@ class AdamW:
 
     def moments(self):
         """What the 8-bit moments stand for: two lists of bf16 tensors."""
-        self._check_places()
         torch, params = self._t[:2]
+        now = list(map(self._address_of, params))
+        if now != self._params_at:
+            self._refuse_moved(now)
         _, here, stream = _on_device(params[0])
         if self._room is None:        # every tensor's place in one buffer, at a multiple of eight elements; the pieces it is cut into, those that are no gaps
             pieces, places, starts, at = [], [], [], 0
