@@ -463,7 +463,8 @@ const char* sb_static_last_error(void);
  * work on `stream` and may be captured into a graph (make the first call on a device outside of a capture: it looks up addresses and raises
  * kernel limits).  A workspace belongs to its call until the work has run: two calls that run at the same time, replays of graphs
  * included, need one each.  rows = 0 is a valid call: gradients of weights are then zero.  The bounded waits inside the kernels report
- * to one status word per device, which sb_ops_check reads.  Errors: return code and sb_last_error().
+ * to one status word per device, which sb_ops_check reads.  No output overlaps another or an input, unless it says so below.  Errors: return code and
+ * sb_last_error().
  */
 
 /* Synchronises `stream`; SB_ERR_TIMEOUT if an operator's kernel has given up on a bounded wait since the last check (the word is then cleared). */
@@ -471,7 +472,7 @@ sb_status sb_ops_check(void* stream);
 
 /*
  * Gated feed-forward block:  GU = X Wgu^T, G and U its left and right halves, H = a(G) * U, Y = H Wd^T.
- *   x [rows, d], w_gate_up [2f, d] (gate rows first), w_down [d, f], y [rows, d]; all 16-byte aligned.
+ *   x [rows, d], w_gate_up [2f, d] (gate rows first), w_down [d, f], y [rows, d]; all 16-byte aligned, at odd widths too.
  *   gu [rows, 2f] : receives GU for the backward pass, or NULL.
  * Backward, from the gradient dy of Y and the GU kept by the forward call:
  *   dH = dY Wd, dG = dH U a'(G), dU = dH a(G), dX = [dG dU] Wgu, dWgu = [dG dU]^T X, dWd = dY^T H; any of dx, dw_gate_up and dw_down may be NULL.

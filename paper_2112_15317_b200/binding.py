@@ -248,7 +248,8 @@ def conv_in_wgrad_static(x, dy, dw, db, precision):
 
 
 # ---- operators on the caller's own tensors ---------------------------------------------------
-# Dense CUDA tensors of one device; outputs and workspaces come from torch's allocator, on the current stream of that device.
+# Dense CUDA tensors of one device (the block's at 16-byte aligned addresses: a slice of rows whose length is odd may not be); outputs and workspaces come
+# from torch's allocator, on the current stream of that device.
 
 
 _here = contextlib.nullcontext()

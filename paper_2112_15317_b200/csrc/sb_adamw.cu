@@ -4,8 +4,8 @@
 //   p <- (1 - lr wd) p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)          (and, where wanted, p's bf16 copy)
 //
 // What bounds it: HBM.  A parameter moves 28 bytes with float moments and gradients, 14 with 8-bit moments and bf16 gradients (plus 2 for
-// the bf16 copy).  129 M parameters with their copy take 601 us (6.4 TB/s) and 347 us (5.9): the second moves half as much for some 60 instructions an
-// element, so that a warp fetches its next block before it works on one (395 us without).  A warp walks blocks of 256 elements, eight consecutive ones a lane, which is also the block that shares a scale of the
+// the bf16 copy).  138 M parameters (VGG-16, 32 tensors) with their copy take 656 us (6.3 TB/s) and 429 us (5.2): the second moves half as much for some 60
+// instructions an element, so that a warp fetches its next block before it works on one (446 us without).  A warp walks blocks of 256 elements, eight consecutive ones a lane, which is also the block that shares a scale of the
 // 8-bit states: its largest magnitudes are one redux instruction, and nothing crosses the warp otherwise.  The tensors' pointers
 // travel as kernel parameters, so that a call needs no table in device memory and can be captured into a graph as it is.
 //
@@ -65,7 +65,7 @@ __device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint32_t c2, u
 }
 
 // Eight consecutive elements from i on, n of the tensor in all: one access where the whole run is there and aligned (floats: 32 bytes; two of 16 bytes for
-// each took 697 us where this takes 650, 129 M parameters with a bf16 copy).
+// each take 672 us where this takes 656, 138 M parameters with a bf16 copy).
 __device__ __forceinline__ void load8(const float* p, int64_t i, int64_t n, bool vec, float (&o)[8])
 {
     if (vec && i + 8 <= n) {
@@ -395,7 +395,7 @@ template <int N>
 cudaError_t launch_list(AdamwArgs<N>& a, int bits, bool bf16_grad, bool moments, cudaStream_t st)
 {
     const int64_t want = (a.blocks + ADAMW_THREADS / 32 - 1) / (ADAMW_THREADS / 32);
-    // (129 M parameters with a bf16 copy, CTAs an SM: 8-bit moments, of which three fit at a time, 8: 372 us, 12: 347, 16: 354; float ones 625, 621, 601)
+    // (138 M parameters with a bf16 copy, CTAs an SM: 8-bit moments, of which three fit at a time, 8: 444 us, 12: 429, 16: 427; float ones 678, 674, 656)
     const int64_t most = 148 * (bits == 8 && !moments ? 12 : 16);
     const dim3 grid((unsigned)(want < most ? want : most)), block(ADAMW_THREADS);
     if (moments) return pdl_launch(adamw_moments_kernel<N>, grid, block, 0, st, a);

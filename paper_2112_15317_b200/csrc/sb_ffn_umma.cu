@@ -14,8 +14,8 @@
 // leave them to TMA stores, which also cut off what lies outside of the matrix.
 //
 // What bounds it: the tensor pipe, busy for 80 % (first product), 88 % (second) and 91 % (dX, dWgu, dWd) of the time, under the power cap when it lasts:
-// 8192 rows, 4096 x 8192, forward 1095 to 1290 us (1.5 to 1.28 PFLOP/s, as a plain library product of the same operands in the same state), 4000 rows backward
-// 1123 to 1310.  The derivative product (tensor pipe 62 %): the shared-memory port, which G, U, dG, dU and H pass beside the MMA's operands.  All waits are bounded and report through the operators' status word.
+// 8192 rows, 4096 x 8192, forward 1095 to 1300 us (1.5 to 1.27 PFLOP/s), 4000 rows backward 1123 to 1340.  In turn with a library's plain products of the
+// same operands: forward 1175 us here and 1214 there, 4000 rows 644 and 622, backward 1246 and 1254.  The derivative product (tensor pipe 62 %): the shared-memory port, which G, U, dG, dU and H pass beside the MMA's operands.  All waits are bounded and report through the operators' status word.
 #include "sb_ffn.h"
 #include "sb_ffn_umma.h"
 #include "sb_tcgen05.cuh"
